@@ -145,7 +145,7 @@ def work(case):
         return {"bytes": 16 * b + rows * (4 + 4 + 4 + 8) + 4 * int(_blocks(case, tail, n_new).sum()), "flops": 0}
     if case["kind"] == "accept":
         rows = b * case["nodes"]
-        return {"bytes": rows * (4 + 8 + 4 + 4 + 4) + 16 * b, "flops": 0}
+        return {"bytes": rows * (4 + 4 + 4 + 4) + 12 * b, "flops": 0}
     row = case["kv_heads"] * case["head_dim"] * 4                # K and V
     if case["kind"] == "append":
         rng = _rng(case)
@@ -237,7 +237,7 @@ def prepare(case, seed):
         right = (vals.random((batch, nodes)) < 0.75) & (parent >= 0)
         rows, cols = np.nonzero(right)
         target[rows, parent[rows, cols]] = token[rows, cols]
-        s.update(n_new=_dev(n_new), parent=_dev(parent), mask=_dev(_bits(_ancestors(parent))), token=_dev(token), target=_dev(target),
+        s.update(n_new=_dev(n_new), parent=_dev(parent), token=_dev(token), target=_dev(target),
                  accept=torch.full((batch, nodes), -1, dtype=I32, device="cuda"), n_accept=torch.zeros(batch, dtype=I32, device="cuda"),
                  next=torch.zeros(batch, dtype=I32, device="cuda"))
         return s
@@ -308,7 +308,7 @@ def _own_attend(s):
 
 def _own_accept(s):
     from paper_2510_18546_b200 import enl
-    enl.enl_tree_accept(s["parent"], s["mask"], s["token"], s["target"], s["accept"], s["n_accept"], s["next"], n_new=s["n_new"], stream=_stream())
+    enl.enl_tree_accept(s["parent"], s["token"], s["target"], s["accept"], s["n_accept"], s["next"], n_new=s["n_new"], stream=_stream())
     return {k: s[k] for k in ("accept", "n_accept", "next")}
 
 
@@ -385,7 +385,7 @@ def _plain_accept(s):
     hit = torch.where(parent < 0, at == 0, said == token) & live
     twin = (parent[:, :, None] == parent[:, None, :]) & hit[:, None, :] & (at[:, None] > at)      # an equal sibling with a lower index
     hit = hit & ~twin.any(2)
-    anc = ((s["mask"][:, :, None] >> at) & 1).bool()
+    anc = _closure(parent, nodes)
     held = (~anc | hit[:, None, :]).all(2) & live
     n = held.sum(1)
     order = torch.where(held, at, nodes).sort(1).values
