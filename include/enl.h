@@ -334,6 +334,133 @@ int enl_select_knapsack(int32_t n, const float *prob, float threshold, const int
 int enl_rope_rotate(void *rows, int32_t n, int32_t n_heads, int32_t head_dim, const int32_t *positions,
                     int32_t first_pos, double base, int32_t interleaved, void *cuda_stream);
 
+/* ---- drafted trees over a growing tail ------------------------------------------------------------- */
+
+/*
+ * While a planner answers (App. C, App. A), every request has keys of its own behind the selected groups: instruction, trajectory and
+ * the tokens answered so far, its TAIL.  The paper writes one token at a time; these four calls also verify several drafted
+ * ones at once, a tree of them per request, and keep every length on the device, so that a step can be captured into a
+ * graph once and replayed while the tails grow:
+ *   enl_tail_tables   block tables, slots and positions of the new rows, ancestor masks of the trees
+ *   enl_attend_tree   the nodes over the selected groups, the tail and their ancestors (per layer)
+ *   enl_tree_accept   which drafted tokens the model would have written itself
+ *   enl_tail_append   their K and V, all layers, into the tail
+ * A tail lies in pages of 16 rows that the caller owns, per layer and for K and V [n_pages][n_kv_heads][16][head_dim] bf16 (the format of
+ * the library's own pages); row i of request b is row i % 16 of page block_table[b][i / 16].  The requests' new rows ("nodes") are
+ * [batch][n_max][...], of which request b has n_new[b].  With n_max = 1 this is the decoding of single tokens.
+ * All arrays are DEVICE memory, int32 unless stated, read and written in stream order.  Every call may be captured.
+ */
+#define ENL_TREE_MAX_NODES  64                       /* nodes of a tree: bits of a mask              */
+#define ENL_TAIL_MAX_BATCH  1024                     /* requests per call of enl_tail_tables         */
+#define ENL_TAIL_MAX_ROWS   16384                    /* n_max of enl_tail_tables and enl_tail_append */
+
+typedef struct {
+    int32_t batch, n_max;              /* requests; rows of the arrays per request                  */
+    int32_t max_blocks;                /* columns of block_table                                    */
+    int32_t n_pages;                   /* entries of free_pages (its capacity)                      */
+    const int32_t *tail_len;           /* [batch] rows of every tail; below zero: the request has ended */
+    const int32_t *n_new;              /* [batch] new rows, or NULL: n_max each                     */
+    const int32_t *parent;             /* [batch][n_max] the node a node continues, a lower index, or -1: it continues */
+                                       /*   the tail; or NULL: every node continues the one before  */
+    const int32_t *pos_base;           /* [batch] position of row 0 of the tail, or NULL: 0         */
+    int32_t *block_table;              /* [batch][max_blocks] in / out                              */
+    int32_t *n_blocks;                 /* [batch] pages that a request holds, in / out              */
+    int32_t *free_pages;               /* [n_pages] stack of the pages that nobody holds, in / out  */
+    int32_t *n_free;                   /* [1] how many there are, in / out                          */
+    int32_t *slot;                     /* [batch][n_max] out: page * 16 + row within it of every new row, -1 behind n_new */
+    int32_t *position;                 /* [batch][n_max] out or NULL: pos_base + tail_len + depth in the tree (rows without */
+                                       /*   `parent`: their index); 0 behind n_new                  */
+    uint64_t *mask;                    /* [batch][n_max] out or NULL: bit j of node i says that j is i or one of its */
+                                       /*   ancestors; 0 behind n_new.  n_max <= ENL_TREE_MAX_NODES  */
+    int32_t *failed;                   /* [1] or NULL: the requests that got no pages are ADDED up here */
+} enl_tail_tables_args_t;
+
+/*
+ * Makes room for the next rows of every request: a request holds ceil((tail_len + n_new) / 16) pages or more afterwards, taken from the
+ * end of free_pages in the order of the requests.  A request that needs more than max_blocks pages, or for which the list does not
+ * last (it and every later one that needs some), gets none and keeps those it has: its slots are -1 and it is counted in
+ * `failed`.  A request whose tail_len is below zero gives its pages back (to the end of the list, behind all that is taken) and has
+ * no new rows.  Counts are taken as between 0 and n_max, a parent that is no lower index as -1.  Entries of block_table
+ * behind a request's pages are left as they are.
+ * Enqueued on the stream; allocates nothing.  Errors: ENL_E_INVAL (null pointer, bad shape), ENL_E_LIMIT (batch beyond ENL_TAIL_MAX_BATCH,
+ * n_max beyond ENL_TAIL_MAX_ROWS, or beyond ENL_TREE_MAX_NODES with `parent` or `mask`, pages whose slots pass 32 bits), ENL_E_CUDA.
+ */
+int enl_tail_tables(const enl_tail_tables_args_t *args, void *cuda_stream);
+
+typedef struct {
+    int32_t layer, batch, n_max;       /* n_max <= ENL_TREE_MAX_NODES                               */
+    const int32_t *sel_ids;            /* HOST [n_sel]: selected group ids, request by request      */
+    const int32_t *cu_sel;             /* HOST [batch+1] prefix counts into sel_ids, or NULL when batch == 1 */
+    int32_t n_sel;
+    int32_t max_blocks, n_pages;       /* columns of block_table; pages of k_tail and v_tail        */
+    const int32_t *tail_len;           /* device [batch]                                            */
+    const int32_t *n_new;              /* device [batch] nodes, or NULL: n_max each                 */
+    const uint64_t *mask;              /* device [batch][n_max]: node i sees node j if bit j is set (its own bit as any */
+                                       /*   other; bits from n_new on count for nothing), or NULL: a chain, j <= i */
+    const int32_t *block_table;        /* device [batch][max_blocks]                                */
+    const void *q;                     /* device bf16 [batch][n_max][n_q_heads][head_dim]           */
+    const void *k_new, *v_new;         /* device bf16 [batch][n_max][n_kv_heads][head_dim]          */
+    const void *k_tail, *v_tail;       /* device bf16 [n_pages][n_kv_heads][16][head_dim]: this layer's */
+    void *out;                         /* device bf16 [batch][n_max][n_q_heads][head_dim]           */
+} enl_attend_tree_args_t;
+
+/*
+ * For every request b, node i < n_new[b] and q head:
+ *   keys = the stored rows of the request's selected groups, the first tail_len[b] rows of its tail, and the nodes that mask[b][i] names;
+ *   out  = softmax(q . keys / sqrt(head_dim)) . values         (fp32 accumulate, bf16 out)
+ * A node that sees no key at all gets zeros.  Rows of `out` behind n_new[b], and those of a request whose tail_len is below zero, are
+ * left as they are.  What lies in rows that do not count (behind a tail's end or the last node) may be anything; the V rows of the
+ * request's own nodes have to be finite, those that a node does not see too.  A tail is taken to be max_blocks * 16 rows long at most, and an entry of the
+ * block table that names no page reads as rows of zeros.  No masses: scoring is enl_attend's.
+ * Limits on the select list are those of enl_attend.  Splits share the cache's scratch buffer: order the calls on one cache.
+ * Errors: ENL_E_INVAL, ENL_E_NOGROUP, ENL_E_EVICTED, ENL_E_NOMEM (plan larger than the plan buffers), ENL_E_LIMIT (n_max, sizes that pass
+ * 32 bits), ENL_E_CUDA.  Kernel-side bounded waits report through enl_cache_status.
+ */
+int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *args, void *cuda_stream);
+
+typedef struct {
+    int32_t batch, n_max;              /* n_max <= ENL_TREE_MAX_NODES                               */
+    const int32_t *n_new;              /* [batch] nodes, or NULL: n_max each                        */
+    const int32_t *parent;             /* [batch][n_max] as in enl_tail_tables, or NULL: a chain    */
+    const int32_t *token;              /* [batch][n_max] drafted tokens                             */
+    const int32_t *target;             /* [batch][n_max] the token that the model puts behind every node */
+    const int32_t *first;              /* [batch] the token that it put behind the tail, or NULL: node 0 is that token */
+    int32_t *accept;                   /* [batch][n_max] out: accepted nodes in ascending order, then -1 */
+    int32_t *n_accept;                 /* [batch] out                                               */
+    int32_t *next;                     /* [batch] out: target of the last accepted node; with none, first[b] or -1 */
+} enl_tree_accept_args_t;
+
+/*
+ * Which drafted tokens the model would have written itself: a node holds if its token is the target of its parent (of several such
+ * children of one parent the lowest index), a node without a parent if its token is first[b] (without `first`: if it is node 0); a node is accepted if it and all its ancestors
+ * hold.  The accepted nodes are one path.  Enqueued on the stream; allocates nothing.
+ * Errors: ENL_E_INVAL, ENL_E_LIMIT (n_max), ENL_E_CUDA.
+ */
+int enl_tree_accept(const enl_tree_accept_args_t *args, void *cuda_stream);
+
+typedef struct {
+    int32_t n_layers, batch, n_max;
+    int32_t n_kv_heads, head_dim;      /* head_dim a multiple of 8                                  */
+    int32_t n_pages;                   /* pages of every k_tail[l], v_tail[l]                       */
+    const void *const *k_new, *const *v_new;   /* HOST [n_layers] device bf16 [batch][n_max][n_kv_heads][head_dim] */
+    void *const *k_tail, *const *v_tail;       /* HOST [n_layers] device bf16 [n_pages][n_kv_heads][16][head_dim] */
+    const int32_t *slot;               /* [batch][n_max] from enl_tail_tables                       */
+    const int32_t *accept;             /* [batch][n_max] rows to append, in order, or NULL: 0, 1, ... */
+    const int32_t *n_accept;           /* [batch] how many, or NULL: n_max each                     */
+    const int32_t *tail_len;           /* [batch]                                                   */
+    int32_t *tail_len_out;             /* [batch] out: tail_len + rows appended; may be tail_len itself */
+} enl_tail_append_args_t;
+
+/*
+ * Row accept[b][k] of k_new[l], v_new[l] goes to slot[b][k], for k < n_accept[b] and every layer; the length grows by as much.  A slot or
+ * a row that is out of range is passed over and does not count (a request that got no pages appends nothing).  A request whose
+ * tail_len is below zero is left alone.  Other rows of the pages are not written.  Two requests must not share slots.
+ * Pointer arrays are consumed before the call returns.  Enqueued on the stream, ENL_TAIL_LAYERS layers a launch; allocates nothing.
+ * Errors: ENL_E_INVAL, ENL_E_LIMIT (n_max, batch, pages whose slots pass 32 bits), ENL_E_CUDA.
+ */
+#define ENL_TAIL_LAYERS     64
+int enl_tail_append(const enl_tail_append_args_t *args, void *cuda_stream);
+
 /* ---- an entry point that allocates nothing ------------------------------------------------ */
 
 #define ENL_STATIC_MAX_SEGMENTS  255                 /* cached segments per call                      */

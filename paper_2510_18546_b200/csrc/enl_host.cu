@@ -6,39 +6,11 @@
 #include <new>
 #include <vector>
 
-#include "../../include/enl.h"
-#include "enl_internal.h"
+#include "enl_cache.h"
 
 using namespace enl;
 
 namespace {
-
-struct Group {
-    std::vector<int32_t> pages;       // shared by all layers: positions 16*i .. 16*i+15 live in pages[i]
-    std::vector<int32_t> len;         // per layer, -1 = never stored
-    // slow tier (Sec. 3.2): pages in the pinned host pool, and which copy is current
-    std::vector<int32_t> host_pages;
-    bool resident = true;             // the device pages hold the group
-    bool host_current = false;        // the host pages hold what the device pages held when last written back
-    uint64_t last_use = 0;            // tick of the last enl_step_prepare that selected the group
-};
-
-struct DeviceGuard {
-    int prev = -1;
-    bool switched = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (dev < 0) return;
-        if (cudaGetDevice(&prev) == cudaSuccess && prev != dev) {
-            cudaSetDevice(dev);
-            switched = true;
-        }
-    }
-    ~DeviceGuard()
-    {
-        if (switched) cudaSetDevice(prev);
-    }
-};
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                    const cuuint64_t *, const cuuint32_t *, const cuuint32_t *,
@@ -58,8 +30,9 @@ EncodeTiledFn get_encode_fn()
     return fn;
 }
 
-// bf16 tensor map with 128-byte swizzle; dims/box innermost first, strides in bytes for dims 1..rank-1.
-bool encode_map(CUtensorMap *tm, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
+}  // namespace
+
+bool enl::encode_map(CUtensorMap *tm, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides,
                 const cuuint32_t *box)
 {
     EncodeTiledFn fn = get_encode_fn();
@@ -70,166 +43,11 @@ bool encode_map(CUtensorMap *tm, const void *base, int rank, const cuuint64_t *d
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
-
-// Tensor maps of the caller's tensors, kept by what they are made from: a planning step calls enl_attend once per layer with
-// tensors that come back step after step, and encoding three maps per call is most of the host time of a call whose
-// gather plan is reused.
-// The key is all that a map is made from.
-struct MapKey {
-    const void *base;
-    cuuint64_t dims[4], strides[3];
-    cuuint32_t box[4];
-    int rank;
-    MapKey() : base(nullptr), dims{}, strides{}, box{}, rank(0) {}
-    MapKey(const void *b, int r, const cuuint64_t *d, const cuuint64_t *s, const cuuint32_t *x) : MapKey()
-    {
-        base = b;
-        rank = r;
-        for (int i = 0; i < r; ++i) { dims[i] = d[i]; box[i] = x[i]; }
-        for (int i = 0; i + 1 < r; ++i) strides[i] = s[i];
-    }
-    bool operator==(const MapKey &o) const
-    {
-        return base == o.base && rank == o.rank && std::equal(dims, dims + 4, o.dims) && std::equal(strides, strides + 3, o.strides) &&
-               std::equal(box, box + 4, o.box);
-    }
-};
-struct MapCache {
-    static constexpr int kSlots = 256;
-    MapKey key[kSlots];
-    CUtensorMap map[kSlots];
-    bool used[kSlots] = {};
-    uint32_t turn = 0;
-    // bf16 map [..][d2][d1][d0] of rank 3 or 4 with box {b0, b1, b2, ..}
-    bool get(CUtensorMap *out, const void *base, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box, int rank = 3)
-    {
-        const MapKey k(base, rank, dims, strides, box);
-        const size_t h = (reinterpret_cast<uintptr_t>(base) >> 8) * 0x9E3779B97F4A7C15ull >> 56;
-        int victim = -1;                                    // the same tensor with another length (decoding), else a free slot
-        for (int probe = 0; probe < 4; ++probe) {
-            const int i = static_cast<int>((h + probe) % kSlots);
-            if (used[i] && key[i] == k) { *out = map[i]; return true; }
-            if (victim < 0 && (!used[i] || key[i].base == base)) victim = i;
-        }
-        if (!encode_map(out, base, rank, dims, strides, box)) return false;
-        const int i = victim >= 0 ? victim : static_cast<int>((h + (turn++ & 3u)) % kSlots);
-        key[i] = k;
-        map[i] = *out;
-        used[i] = true;
-        return true;
-    }
-};
-
-// a caller's [n][Hkv][D] keys or values, fetched by a few rows of a head
-struct KeyMapShape {
-    cuuint64_t dims[4], strides[3];
-    cuuint32_t box[4];
-    KeyMapShape(int D, int Hkv, int n)
-        : dims{64, static_cast<cuuint64_t>(n), static_cast<cuuint64_t>(D / 64), static_cast<cuuint64_t>(Hkv)},
-          strides{static_cast<cuuint64_t>(D) * 2 * Hkv, 128, static_cast<cuuint64_t>(D) * 2},
-          box{64, static_cast<cuuint32_t>(box_rows(D)), static_cast<cuuint32_t>(D / 64), 1} {}
-};
-
-}  // namespace
-
 bool enl::encode_key_map(CUtensorMap *tm, const void *base, int D, int Hkv, int n)
 {
     const KeyMapShape k(D, Hkv, n);
     return encode_map(tm, base, 4, k.dims, k.strides, k.box);
 }
-
-struct enl_cache {
-    enl_cache_desc_t d{};
-    bool gpu = false;
-    int rep = 1;
-    int n_sm = 148;                         // multiprocessors of the device (grid sizes, split counts)
-    int64_t n_pages = 0;
-    size_t layer_bytes = 0;                 // one layer of one pool
-    uint8_t *work = nullptr;                // the device allocation that holds all but the pools
-    uint8_t *kpool = nullptr, *vpool = nullptr;
-    std::vector<int32_t> free_pages;        // stack of free page ids (page 0 is never in it)
-    std::vector<Group> groups;
-    std::vector<CUtensorMap> tm_k, tm_v;    // per layer
-    uint64_t epoch = 0;                     // bumped by every store
-
-    // gather plan: host image (pinned when there is a GPU), device copy, capacities
-    int32_t cap_entries = 0, cap_items = 0;
-    uint8_t *plan_host = nullptr, *plan_dev = nullptr;
-    // sections of the current plan, back to back in the order of their offsets
-    size_t off_eps = 0, off_items = 0, off_stream = 0, off_meta = 0, off_rowslots = 0, off_rowobj = 0, off_chg = 0, plan_used = 0;
-    size_t plan_bytes = 0;                  // capacity
-    cudaEvent_t plan_copied = nullptr;
-    bool plan_copying = false;              // a copy out of plan_host may be under way (until plan_copied)
-    bool plan_valid = false, plan_on_device = false;
-    std::vector<uint8_t> plan_layer_ok;     // layers whose group lengths have been compared with the plan's
-    std::vector<int32_t> sel_len;           // working space of a call
-    uint64_t plan_epoch = 0;
-    int32_t plan_split_hint = 0;
-    bool plan_has_mass = false;
-    bool plan_mass_only = false, plan_sums = false;      // what the call wants besides or instead of outputs
-    bool plan_park = false;                 // every CTA walks few slots: it parks their sums in shared memory and writes the masses itself
-    bool plan_finish = false;               // else a kernel behind the attention kernel turns log-sums into masses
-    std::vector<int32_t> key_obj;           // object spans the row -> object map was built from
-    bool plan_decode = false;               // the plan is for the one-token decode kernel
-    int32_t plan_small_blocks = 0;          // > 0: the plan is for the kernel of short calls, with this many row blocks per kv head
-    int32_t plan_small_groups = 0;          // ... of this many times 16 rows
-    int32_t plan_cluster = 0;               // decode: CTAs per cluster, 0 = the streaming kernel
-    int32_t plan_list_pages = 0;            // decode by clusters: most pages one of the CTAs covers
-    ClusterCaps cluster_caps = {};          // decode by clusters: how many run at once (none on a bookkeeping-only cache)
-    // Order of launches, outside captures: a launch that writes the plan or the pool has been enqueued since the last attention
-    // launch.  What a capture records runs when its graph does, so calls inside one go by what the same capture holds.
-    bool written = true;
-    unsigned long long settled_graph = 0;   // capture that holds an attention launch behind everything written so far
-    unsigned long long plan_graph = 0;      // capture that holds the write of the current plan
-    bool plan_in_graphs = false;            // some graph may write its plan over the one on the device at any time
-    bool pool_in_graphs = false;            // some graph holds launches that write the pool: it may run before any call outside it
-    bool plan_pair = false;                 // two splits whose CTAs merge inside the attention kernel (cluster of two)
-    bool plan_halves = false;               // items of one Q tile whose steps the two halves of a CTA share
-    bool pairs_ok = false;                  // the device can co-schedule two of the attention kernel's CTAs as a cluster
-    std::vector<int32_t> key_sel, key_cu, key_len;   // what the current plan was built from
-    int32_t plan_entries = 0, plan_items = 0, plan_splits = 1, plan_batch = 0, plan_max_slots = 0;
-    MapCache maps;                          // tensor maps of the caller's q / k_new / v_new
-    std::vector<int32_t> seen;              // duplicate detection stamps
-    int32_t stamp = 0;
-
-    // slow tier
-    bool tier = false;
-    int64_t n_host_pages = 0;
-    size_t host_layer_bytes = 0;
-    uint8_t *host_k = nullptr, *host_v = nullptr;           // pinned, [layer][page][kv head][16][D]
-    std::vector<int32_t> free_host_pages;
-    int2 *pairs_host = nullptr, *pairs_dev = nullptr;        // page moves of one enqueue (pinned staging + device copy)
-    int32_t cap_pairs = 0;
-    cudaEvent_t pairs_copied = nullptr;
-    // loads of several megabytes run beside the caller's stream, a few layers at a time (see enqueue_loads)
-    cudaStream_t load_stream[2] = {nullptr, nullptr};
-    std::vector<cudaEvent_t> load_done;                     // per chunk of layers
-    int load_chunks = 0, load_layers = 1;                   // chunks not known to be complete (0: none pending), layers of a chunk
-    uint64_t tick = 0;
-
-    float *scratch = nullptr;
-    float *finish_lse = nullptr;            // rows' log-sum-exps for that kernel, and the splits' parts of shared slots
-    float2 *finish_bnd = nullptr;
-    int64_t finish_cap = 0;                 // entries of either
-    int32_t *status_dev = nullptr;
-    int32_t *counters_dev = nullptr;        // decode: finished splits per (episode, kv head)
-
-    EpInfo *h_eps() { return reinterpret_cast<EpInfo *>(plan_host + off_eps); }
-    Item *h_items() { return reinterpret_cast<Item *>(plan_host + off_items); }
-    int32_t *h_stream() { return reinterpret_cast<int32_t *>(plan_host + off_stream); }
-    int32_t *h_meta() { return reinterpret_cast<int32_t *>(plan_host + off_meta); }
-    int32_t *h_rowslots() { return reinterpret_cast<int32_t *>(plan_host + off_rowslots); }
-    uint8_t *h_chg() { return plan_host + off_chg; }
-    // A launch that writes the pool is about to be enqueued (captured: a graph that does so is being made).
-    void pool_written(bool captured)
-    {
-        written = true;
-        settled_graph = 0;
-        pool_in_graphs = pool_in_graphs || captured;
-    }
-    int32_t *h_rowobj() { return reinterpret_cast<int32_t *>(plan_host + off_rowobj); }
-};
 
 namespace {
 
@@ -363,14 +181,10 @@ extern "C" int enl_cache_create(const enl_cache_desc_t *desc, enl_cache_t **out)
 
     c->tm_k.resize(d.n_layers);
     c->tm_v.resize(d.n_layers);
-    const cuuint64_t row = static_cast<cuuint64_t>(d.head_dim) * 2;
-    const cuuint32_t group = box_rows(d.head_dim), page_groups = kPageTokens / group;
-    const cuuint64_t dims[4] = {64, group, static_cast<cuuint64_t>(d.head_dim / 64), static_cast<cuuint64_t>(c->n_pages) * d.n_kv_heads * page_groups};
-    const cuuint64_t strides[3] = {row, 128, row * group};
-    const cuuint32_t box[4] = {64, group, static_cast<cuuint32_t>(d.head_dim / 64), page_groups};
+    const PageMapShape pm(d.head_dim, d.n_kv_heads, c->n_pages);
     for (int l = 0; l < d.n_layers; ++l) {
-        if (!encode_map(&c->tm_k[l], c->kpool + c->layer_bytes * l, 4, dims, strides, box) ||
-            !encode_map(&c->tm_v[l], c->vpool + c->layer_bytes * l, 4, dims, strides, box)) {
+        if (!encode_map(&c->tm_k[l], c->kpool + c->layer_bytes * l, 4, pm.dims, pm.strides, pm.box) ||
+            !encode_map(&c->tm_v[l], c->vpool + c->layer_bytes * l, 4, pm.dims, pm.strides, pm.box)) {
             destroy(c);
             return ENL_E_CUDA;
         }
@@ -399,10 +213,8 @@ extern "C" int32_t enl_group_len(const enl_cache_t *c, int32_t group_id, int32_t
     return g.len.empty() ? -1 : g.len[layer];
 }
 
-namespace {
-
 // The capture that `st` is in, 0 = none (a graph's launches run when the graph does, not now).
-unsigned long long capture_of(cudaStream_t st)
+unsigned long long enl::capture_of(cudaStream_t st)
 {
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     unsigned long long id = 0;
@@ -411,7 +223,7 @@ unsigned long long capture_of(cudaStream_t st)
 }
 
 // Waits on the host for an event that was recorded outside any capture; legal while a stream is being captured.
-bool host_waits(cudaEvent_t e)
+static bool host_waits(cudaEvent_t e)
 {
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     bool ok = cudaThreadExchangeStreamCaptureMode(&mode) == cudaSuccess;
@@ -424,7 +236,7 @@ bool host_waits(cudaEvent_t e)
 }
 
 // Puts work of `st` that is about to be enqueued behind the loads that are still under way: those of one layer, or (-1) all.
-int join_loads(enl_cache *c, cudaStream_t st, int layer)
+int enl::join_loads(enl_cache *c, cudaStream_t st, int layer)
 {
     if (c->load_chunks == 0) return ENL_OK;
     const int last = c->load_chunks - 1, other = std::max(0, last - 1);       // the last chunk of either load stream
@@ -445,8 +257,6 @@ int join_loads(enl_cache *c, cudaStream_t st, int layer)
     if (!ok) { cudaGetLastError(); return ENL_E_CUDA; }
     return ENL_OK;
 }
-
-}  // namespace
 
 extern "C" int enl_cache_status(enl_cache_t *c)
 {
@@ -624,6 +434,83 @@ extern "C" int enl_group_store_all_layers(enl_cache_t *c, int32_t group_id, int3
     return ENL_OK;
 }
 
+int enl::look_over(enl_cache *c, int layer, int B, const int32_t *sel_ids, const int32_t *cu_sel)
+{
+    c->sel_len.resize(cu_sel[B]);
+    for (int b = 0; b < B; ++b) {
+        if (++c->stamp == 0x7fffffff) { std::fill(c->seen.begin(), c->seen.end(), 0); c->stamp = 1; }
+        for (int s = cu_sel[b]; s < cu_sel[b + 1]; ++s) {
+            const int32_t gid = sel_ids[s];
+            if (gid < 0 || gid >= c->d.max_groups) return ENL_E_NOGROUP;
+            const Group &g = c->groups[gid];
+            if (g.len.empty() || g.len[layer] < 0) return ENL_E_NOGROUP;
+            if (!g.resident) return ENL_E_EVICTED;
+            if (c->seen[gid] == c->stamp) return ENL_E_INVAL;
+            c->seen[gid] = c->stamp;
+            c->sel_len[s] = g.len[layer];
+        }
+    }
+    return ENL_OK;
+}
+
+int enl::open_plan(enl_cache *c)
+{
+    if (c->plan_copying) {
+        if (!host_waits(c->plan_copied)) return ENL_E_CUDA;
+        c->plan_copying = false;
+    }
+    c->plan_valid = false;
+    return ENL_OK;
+}
+
+int32_t enl::write_stream(enl_cache *c, EpInfo &e, const int32_t *ids, const int32_t *lens, int32_t ne)
+{
+    int32_t *stream = c->h_stream(), *smeta = c->h_meta();
+    e.stream_off = ne;
+    for (int slot = 0; slot < e.n_slots; ++slot) {
+        const Group &g = c->groups[ids[slot]];
+        const int len = lens[slot], np = ceil_div(len, kPageTokens);
+        if (np == 0) { stream[ne] = kZeroPage; smeta[ne++] = slot << 8; }
+        for (int i = 0; i < np; ++i) {
+            const int nv = std::min(kPageTokens, len - i * kPageTokens);
+            stream[ne] = g.pages[i];
+            smeta[ne++] = (slot << 8) | nv;
+        }
+    }
+    e.n_entries = ne - e.stream_off;
+    while ((ne - e.stream_off) % kPagesPerTile) { stream[ne] = kZeroPage; smeta[ne++] = (e.n_slots - 1) << 8; }
+    e.n_ctiles = (ne - e.stream_off) / kPagesPerTile;
+    return ne;
+}
+
+// The plan goes to the device with the first launch that uses it: as parameters of a small kernel, or, when it is too
+// large for that (beyond some 3500 pages of 16 tokens), as one copy, before which this buffer must not be rebuilt.
+// A graph that is being captured gets its own writes, as parameters of as many kernels as it takes: it may run at any time, or never.
+int enl::send_plan(enl_cache *c, unsigned long long graph, cudaStream_t st)
+{
+    const bool fresh = graph ? c->plan_graph != graph : !c->plan_on_device || c->plan_in_graphs;
+    if (!fresh) return ENL_OK;
+    bool okc = true;
+    if (graph || c->plan_used <= static_cast<size_t>(kPlanParamBytes)) {
+        for (size_t at = 0; okc && at < c->plan_used; at += kPlanParamBytes)
+            okc = launch_plan_write(c->plan_dev + at, c->plan_host + at, std::min<size_t>(kPlanParamBytes, c->plan_used - at), st) == cudaSuccess;
+    } else {
+        okc = cudaMemcpyAsync(c->plan_dev, c->plan_host, c->plan_used, cudaMemcpyHostToDevice, st) == cudaSuccess &&
+              cudaEventRecord(c->plan_copied, st) == cudaSuccess;
+        c->plan_copying = true;
+    }
+    if (!okc) { cudaGetLastError(); c->plan_valid = false; return ENL_E_CUDA; }
+    if (graph) {
+        c->plan_graph = graph;
+        c->plan_in_graphs = true;
+        c->settled_graph = 0;
+    } else {
+        c->plan_on_device = true;
+        c->written = true;
+    }
+    return ENL_OK;
+}
+
 extern "C" int enl_attend(enl_cache_t *c, const enl_attend_args_t *a, void *cuda_stream)
 {
     if (!c || !a) return ENL_E_INVAL;
@@ -675,7 +562,7 @@ extern "C" int enl_attend(enl_cache_t *c, const enl_attend_args_t *a, void *cuda
     const bool same_obj = has_sum ? c->key_obj.size() == static_cast<size_t>(a->n_obj) + 1 &&
                                         std::memcmp(c->key_obj.data(), a->obj_off, sizeof(int32_t) * (a->n_obj + 1)) == 0
                                   : true;
-    bool reuse = c->plan_valid && c->plan_epoch == c->epoch && c->plan_split_hint == a->split_hint &&
+    bool reuse = c->plan_valid && !c->plan_tree && c->plan_epoch == c->epoch && c->plan_split_hint == a->split_hint &&
                  c->plan_has_mass == has_mass && c->plan_mass_only == mass_only &&
                  c->plan_sums == has_sum && same_obj && c->plan_batch == B &&
                  c->key_sel.size() == static_cast<size_t>(a->n_sel) &&
@@ -689,20 +576,7 @@ extern "C" int enl_attend(enl_cache_t *c, const enl_attend_args_t *a, void *cuda
     // the groups at other lengths.
     std::vector<int32_t> &sel_len = c->sel_len;
     if (!reuse || !c->plan_layer_ok[a->layer]) {
-        sel_len.resize(a->n_sel);
-        for (int b = 0; b < B; ++b) {
-            if (++c->stamp == 0x7fffffff) { std::fill(c->seen.begin(), c->seen.end(), 0); c->stamp = 1; }
-            for (int s = cu_sel[b]; s < cu_sel[b + 1]; ++s) {
-                const int32_t gid = a->sel_ids[s];
-                if (gid < 0 || gid >= d.max_groups) return ENL_E_NOGROUP;
-                const Group &g = c->groups[gid];
-                if (g.len.empty() || g.len[a->layer] < 0) return ENL_E_NOGROUP;
-                if (!g.resident) return ENL_E_EVICTED;
-                if (c->seen[gid] == c->stamp) return ENL_E_INVAL;
-                c->seen[gid] = c->stamp;
-                sel_len[s] = g.len[a->layer];
-            }
-        }
+        if (const int rc = look_over(c, a->layer, B, a->sel_ids, cu_sel)) return rc;
         reuse = reuse && c->key_len == sel_len;
         if (reuse) c->plan_layer_ok[a->layer] = 1;
     }
@@ -885,11 +759,7 @@ extern "C" int enl_attend(enl_cache_t *c, const enl_attend_args_t *a, void *cuda
             while (n_splits > 1 && !mass_only && !fits(n_splits)) --n_splits;
         }
 
-        if (c->plan_copying) {
-            if (!host_waits(c->plan_copied)) return ENL_E_CUDA;
-            c->plan_copying = false;
-        }
-        c->plan_valid = false;
+        if (const int rc = open_plan(c)) return rc;
         // Two splits of a head_dim-128 call are launched as clusters of two CTAs, which exchange their partial
         // results through distributed shared memory: no scratch round trip and no merge kernel.  Every CTA must
         // have at least one tile, and the items of a pair must be neighbours (they are: same tile count, stable sort).
@@ -911,32 +781,17 @@ extern "C" int enl_attend(enl_cache_t *c, const enl_attend_args_t *a, void *cuda
             c->plan_used = at;
         }
         EpInfo *eps = c->h_eps();
-        int32_t *stream = c->h_stream();
-        int32_t *smeta = c->h_meta();
+        const int32_t *smeta = c->h_meta();
         int32_t *rowslots = c->h_rowslots();
         int32_t ne = 0;
         for (int b = 0; b < B; ++b) {
             EpInfo &e = eps[b];
-            e.stream_off = ne;
             e.n_slots = cu_sel[b + 1] - cu_sel[b];
             e.q_off = cu_q[b];
             e.n_q = cu_q[b + 1] - cu_q[b];
             e.new_off = cu_new[b];
             e.n_new = cu_new[b + 1] - cu_new[b];
-            for (int s = cu_sel[b]; s < cu_sel[b + 1]; ++s) {
-                const int slot = s - cu_sel[b];
-                const Group &g = c->groups[a->sel_ids[s]];
-                const int len = sel_len[s], np = ceil_div(len, kPageTokens);
-                if (np == 0) { stream[ne] = kZeroPage; smeta[ne++] = slot << 8; }
-                for (int i = 0; i < np; ++i) {
-                    const int nv = std::min(kPageTokens, len - i * kPageTokens);
-                    stream[ne] = g.pages[i];
-                    smeta[ne++] = (slot << 8) | nv;
-                }
-            }
-            e.n_entries = ne - e.stream_off;
-            while ((ne - e.stream_off) % kPagesPerTile) { stream[ne] = kZeroPage; smeta[ne++] = (e.n_slots - 1) << 8; }
-            e.n_ctiles = (ne - e.stream_off) / kPagesPerTile;
+            ne = write_stream(c, e, a->sel_ids + cu_sel[b], sel_len.data() + cu_sel[b], ne);
             for (int j = 0; j < e.n_ctiles && mass_only; ++j) {
                 uint32_t chg = 0;
                 for (int x = 0; x < kPagesPerTile; ++x) {
@@ -987,6 +842,7 @@ extern "C" int enl_attend(enl_cache_t *c, const enl_attend_args_t *a, void *cuda
         c->plan_has_mass = has_mass;
         c->plan_mass_only = mass_only;
         c->plan_sums = has_sum;
+        c->plan_tree = false;
         const bool merged = !decode && n_splits > 1 && !pair && !mass_only;
         c->plan_small_blocks = small_blocks;
         c->plan_small_groups = small_groups;
@@ -1011,39 +867,15 @@ extern "C" int enl_attend(enl_cache_t *c, const enl_attend_args_t *a, void *cuda
     if (plan_only) return ENL_OK;
     if (join_loads(c, st, a->layer) != ENL_OK) return ENL_E_CUDA;
 
-    // The plan goes to the device with the first launch that uses it: as parameters of a small kernel, or, when it is too
-    // large for that (beyond some 3500 pages of 16 tokens), as one copy, before which this buffer must not be rebuilt.
-    // (A short call of one episode takes it along in its own parameters.)  A graph that is being captured gets its own writes,
-    // as parameters of as many kernels as it takes: it may run at any time, or never.
     const unsigned long long graph = capture_of(st);
-    const bool plan_inside = c->plan_small_blocks && c->plan_batch == 1;
-    const bool fresh = !plan_inside && (graph ? c->plan_graph != graph : !c->plan_on_device || c->plan_in_graphs);
-    if (fresh) {
-        bool okc = true;
-        if (graph || c->plan_used <= static_cast<size_t>(kPlanParamBytes)) {
-            for (size_t at = 0; okc && at < c->plan_used; at += kPlanParamBytes)
-                okc = launch_plan_write(c->plan_dev + at, c->plan_host + at, std::min<size_t>(kPlanParamBytes, c->plan_used - at), st) == cudaSuccess;
-        } else {
-            okc = cudaMemcpyAsync(c->plan_dev, c->plan_host, c->plan_used, cudaMemcpyHostToDevice, st) == cudaSuccess &&
-                  cudaEventRecord(c->plan_copied, st) == cudaSuccess;
-            c->plan_copying = true;
-        }
-        if (!okc) { cudaGetLastError(); c->plan_valid = false; return ENL_E_CUDA; }
-        if (graph) {
-            c->plan_graph = graph;
-            c->plan_in_graphs = true;
-            c->settled_graph = 0;
-        } else {
-            c->plan_on_device = true;
-            c->written = true;
-        }
-    }
+    const bool plan_inside = c->plan_small_blocks && c->plan_batch == 1;      // a short call of one episode takes it along in its own parameters
+    if (!plan_inside && send_plan(c, graph, st) != ENL_OK) return ENL_E_CUDA;
     // Launches that find plan and pool as the attention launch before left them may read both before the kernel before them
     // has ended.  Ones that do not wait for it first and hold their own successor back until then, so that this carries over:
     // from an attention launch that was made, not from one that was refused.  A graph that stores may have run right before any call
     // outside it, so once there is one those calls always wait.
     const bool wait_first = graph ? c->settled_graph != graph : c->written || c->pool_in_graphs;
-    auto settled = [&]() { if (graph) c->settled_graph = graph; else c->written = false; };
+    auto settled = [&]() { c->settle(graph); };
 
     const int slot_stride = c->plan_max_slots + 1;
     if (c->plan_small_blocks || (c->plan_decode && c->plan_cluster)) {

@@ -168,6 +168,46 @@ struct StaticDecodeParams {
     int32_t page_off[kStaticMaxSeg + 2];    // the same in pages (16 keys of one slot, the last one of a slot partly filled)
 };
 
+// Drafted trees over selected groups and a growing tail (see enl_tree_sm100.cu)
+struct TreeParams {
+    CUtensorMap tm_q;       // [batch * n_max][Hq][D]   box {64, rep, box_tokens}
+    CUtensorMap tm_knew;    // as in AttnParams, the requests' nodes
+    CUtensorMap tm_vnew;
+    CUtensorMap tm_kpool;   // one layer: a page of a head
+    CUtensorMap tm_vpool;
+    CUtensorMap tm_ktail;   // the caller's tail pages, of the same format
+    CUtensorMap tm_vtail;
+    EpInfo ep0;             // request 0 (used when the call has one)
+    const EpInfo *eps;
+    const int32_t *stream_page;
+    const int32_t *stream_meta;
+    const int32_t *block_table;     // [batch][max_blocks] pages of the tails
+    const int32_t *tail_len;        // [batch]
+    const int32_t *n_new;           // [batch] nodes, or null: n_max
+    const unsigned long long *mask; // [batch][n_max] nodes that a node sees (a bit each), or null: a chain
+    void   *out;            // bf16 [batch][n_max][Hq][D]
+    float  *part_o;         // [CTA][D / 4][128 rows][4] outputs of splits, normalised by their own sums
+    float  *part_lse;       // [CTA][128] their log2-sum-exps
+    int4   *part_head;      // [batch] first CTA, splits, row tiles, nodes (null when the call is not split)
+    int32_t *status;        // as in AttnParams
+    int32_t batch, n_max, max_blocks, n_tail_pages;
+    int32_t Hq, Hkv, rep;
+    int32_t box_tokens;     // tokens of a Q box
+    int32_t may_split;
+    int32_t min_steps;      // a split takes as many steps of 64 keys, at least
+    float   scale_log2;
+};
+struct TreeMergeParams {
+    const float *part_o, *part_lse;
+    const int4 *part_head;
+    void *out;
+    int32_t n_max, Hq, Hkv, rep;
+};
+constexpr int kTreeMaxNodes = 64;   // bits of a mask
+cudaError_t prepare_tree(int head_dim);
+cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_t st);
+cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int row_tiles, int batch, cudaStream_t st);
+
 struct CombineParams {
     const float *part_o, *part_lse, *part_slot;
     const int2 *part_rng;       // [split][row]: first and last slot that the split has written, or null: all are

@@ -1,0 +1,418 @@
+// Tails: block tables and slot maps from the requests' lengths, the accepted path of a drafted tree, rows into tail pages.
+// Everything the calls go by is read on the device, so that a captured step stays valid while the tails grow.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "../../include/enl.h"
+#include "enl_internal.h"
+
+namespace {
+
+using enl::kPageTokens;
+constexpr uint32_t kFull = 0xffffffffu;
+constexpr int kMaxNodes = ENL_TREE_MAX_NODES;
+constexpr int kMaxPages = 0x7fffffff / kPageTokens;       // slots are int32
+static_assert(kMaxNodes == enl::kTreeMaxNodes && kMaxNodes == 64, "two nodes a lane, a 64-bit mask");
+
+// ---- block tables, slots, positions, ancestor masks ----------------------------------------------------------------------
+
+struct TablesParams {
+    const int32_t *tail_len, *n_new, *parent, *pos_base;
+    int32_t *block_table, *n_blocks, *free_pages, *n_free, *slot, *position, *failed;
+    unsigned long long *mask;
+    int32_t batch, n_max, max_blocks, n_pages;
+};
+
+// What comes from the kernel before is read past the L1: this one may have started while that one ran.
+__device__ __forceinline__ int nodes_of(const TablesParams &p, int b, int len)
+{
+    const int n = p.n_new ? __ldcg(p.n_new + b) : p.n_max;
+    return len < 0 ? 0 : max(0, min(n, p.n_max));
+}
+__device__ __forceinline__ int blocks_for(int len, int n)
+{
+    return static_cast<int>((static_cast<long long>(len) + n + kPageTokens - 1) / kPageTokens);
+}
+// sum over the CTA's threads up to and with this one, and over all of them
+__device__ int scan(int x, int *warp_sums, int &total)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    int upto = x;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += t;
+    }
+    if (lane == 31) warp_sums[warp] = upto;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < warps; ++w) {
+        const int t = warp_sums[w];
+        if (w < warp) before += t;
+        total += t;
+    }
+    __syncthreads();
+    return before + upto;
+}
+
+// One CTA, a thread per request: pages are taken from the end of the list in the order of the requests, then those of ended ones go there.
+__device__ void grow(const TablesParams &p, int *warp_sums)
+{
+    const int b = threadIdx.x;
+    const bool on = b < p.batch;
+    const int avail = max(0, min(__ldcg(p.n_free), p.n_pages));
+    int take = 0, give = 0, have = 0;
+    bool failed = false;
+    if (on) {
+        const int len = __ldcg(p.tail_len + b), n = nodes_of(p, b, len);
+        have = max(0, min(__ldcg(p.n_blocks + b), p.max_blocks));
+        if (len < 0) {
+            give = have;
+        } else {
+            const int want = blocks_for(len, n);
+            failed = want > p.max_blocks;
+            take = failed ? 0 : max(0, want - have);
+        }
+    }
+    int wanted, given;
+    const int upto = scan(take, warp_sums, wanted);
+    if (take > 0 && upto > avail) {                         // so it is for every later request that takes some
+        failed = true;
+        take = 0;
+    }
+    int taken;
+    scan(take, warp_sums, taken);
+    int32_t *row = p.block_table + static_cast<long long>(b) * p.max_blocks;
+    for (int k = 0; k < take; ++k) row[have + k] = __ldcg(p.free_pages + (avail - 1 - (upto - take + k)));
+    const int give_upto = scan(give, warp_sums, given);     // (its barriers stand between the last read of the list and the first write)
+    const int top = avail - taken;
+    for (int k = 0; k < give; ++k) {
+        const int at = top + give_upto - give + k;
+        if (at < p.n_pages) p.free_pages[at] = __ldcg(row + k);
+    }
+    if (on) p.n_blocks[b] = give > 0 ? 0 : have + take;
+    const int n_failed = __syncthreads_count(failed);
+    if (threadIdx.x == 0) {
+        *p.n_free = min(top + given, p.n_pages);
+        if (p.failed && n_failed) *p.failed += n_failed;
+    }
+}
+
+// A warp fills 64 rows of one request, two a lane (i = lane and lane + 32 from `row0` on).
+__device__ void fill(const TablesParams &p, int b, int row0)
+{
+    const int lane = threadIdx.x & 31;
+    const int len = __ldcg(p.tail_len + b), n = nodes_of(p, b, len);
+    const bool roomy = n > 0 && static_cast<long long>(__ldcg(p.n_blocks + b)) * kPageTokens >= static_cast<long long>(len) + n;
+    const int base = p.pos_base ? __ldcg(p.pos_base + b) : 0;
+    const long long at = static_cast<long long>(b) * p.n_max;
+    unsigned long long anc[2];
+    int depth[2];
+    if (p.parent) {                                         // n_max <= 64
+        // Every node's ancestors up to 2^round away, and the node beyond them: six rounds reach all 64.
+        int up[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane + 32 * h;
+            up[h] = i < n ? __ldcg(p.parent + at + i) : -1;
+            if (up[h] >= i || up[h] < 0) up[h] = -1;
+            anc[h] = i < n ? 1ull << i : 0ull;
+        }
+#pragma unroll 1
+        for (int round = 0; round < 6; ++round) {
+            unsigned long long a[2];
+            int u[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int from = up[h] & 31;
+                const unsigned long long a0 = __shfl_sync(kFull, anc[0], from), a1 = __shfl_sync(kFull, anc[1], from);
+                const int u0 = __shfl_sync(kFull, up[0], from), u1 = __shfl_sync(kFull, up[1], from);
+                a[h] = up[h] < 0 ? 0ull : up[h] < 32 ? a0 : a1;
+                u[h] = up[h] < 0 ? -1 : up[h] < 32 ? u0 : u1;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                anc[h] |= a[h];
+                up[h] = u[h];
+            }
+        }
+        depth[0] = __popcll(anc[0]) - 1;
+        depth[1] = __popcll(anc[1]) - 1;
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            depth[h] = row0 + lane + 32 * h;
+            anc[h] = depth[h] < n ? (2ull << (depth[h] & 63)) - 1ull : 0ull;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = row0 + lane + 32 * h;
+        if (i >= p.n_max) continue;
+        int s = -1;
+        if (roomy && i < n) {
+            const int r = len + i;
+            s = __ldcg(p.block_table + static_cast<long long>(b) * p.max_blocks + r / kPageTokens) * kPageTokens + r % kPageTokens;
+        }
+        p.slot[at + i] = s;
+        if (p.position) p.position[at + i] = i < n ? base + len + depth[h] : 0;
+        if (p.mask) p.mask[at + i] = anc[h];
+    }
+}
+
+// Bound by the latency of three dependent round trips (counts, free list, table) and two barriers.  Up to kOneCtaWarps warps of rows are filled by the
+// CTA that grows the tables, more by a launch of their own.
+constexpr int kOneCtaWarps = 64;
+__global__ void __launch_bounds__(1024) tables_kernel(const __grid_constant__ TablesParams p, int fill_too)
+{
+    __shared__ int warp_sums[32];
+    enl::pdl_trigger();
+    enl::pdl_wait();
+    grow(p, warp_sums);
+    if (!fill_too) return;
+    __syncthreads();                                        // the tables are there
+    const int chunks = (p.n_max + 63) / 64;
+    for (int i = threadIdx.x >> 5; i < p.batch * chunks; i += blockDim.x >> 5) fill(p, i / chunks, i % chunks * 64);
+}
+__global__ void __launch_bounds__(256) fill_kernel(const __grid_constant__ TablesParams p)
+{
+    enl::pdl_trigger();
+    enl::pdl_wait();
+    const int chunks = (p.n_max + 63) / 64, i = static_cast<int>(blockIdx.x) * 8 + (static_cast<int>(threadIdx.x) >> 5);
+    if (i < p.batch * chunks) fill(p, i / chunks, i % chunks * 64);
+}
+
+// ---- accepted path --------------------------------------------------------------------------------------------------------
+
+struct AcceptParams {
+    const int32_t *n_new, *parent, *token, *target, *first;
+    int32_t *accept, *n_accept, *next;
+    int32_t batch, n_max;
+};
+
+// A warp per request, two nodes a lane.  Whether a node holds is known to its lane at once; the path is then walked with a ballot a
+// node: among the children of the last accepted node that hold the lowest index comes next.
+__global__ void __launch_bounds__(256) accept_kernel(const __grid_constant__ AcceptParams p)
+{
+    enl::pdl_trigger();
+    enl::pdl_wait();
+    const int b = static_cast<int>(blockIdx.x) * static_cast<int>(blockDim.x >> 5) + (static_cast<int>(threadIdx.x) >> 5), lane = threadIdx.x & 31;
+    if (b >= p.batch) return;
+    const long long at = static_cast<long long>(b) * p.n_max;
+    const int n = p.n_new ? max(0, min(__ldcg(p.n_new + b), p.n_max)) : p.n_max;
+    const int first = p.first ? __ldcg(p.first + b) : -1;
+    int up[2], tok[2], tgt[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = lane + 32 * h;
+        const bool on = i < n;
+        up[h] = !on ? -2 : p.parent ? __ldcg(p.parent + at + i) : i - 1;
+        if (on && (up[h] >= i || up[h] < 0)) up[h] = -1;
+        tok[h] = on ? __ldcg(p.token + at + i) : 0;
+        tgt[h] = on ? __ldcg(p.target + at + i) : 0;
+    }
+    bool hit[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int t0 = __shfl_sync(kFull, tgt[0], up[h] & 31), t1 = __shfl_sync(kFull, tgt[1], up[h] & 31);
+        const int i = lane + 32 * h;
+        hit[h] = up[h] == -1 ? (p.first ? tok[h] == first : i == 0) : up[h] >= 0 && tok[h] == (up[h] < 32 ? t0 : t1);
+    }
+    int cur = -1, count = 0, mine[2] = {-1, -1};
+    for (;;) {                                              // ends: the path only goes to higher indices
+        const unsigned lo = __ballot_sync(kFull, hit[0] && up[0] == cur), hi = __ballot_sync(kFull, hit[1] && up[1] == cur);
+        if (!(lo | hi)) break;
+        cur = lo ? __ffs(lo) - 1 : 31 + __ffs(hi);
+        if (count == lane) mine[0] = cur;
+        if (count == lane + 32) mine[1] = cur;
+        ++count;
+    }
+    const int t0 = __shfl_sync(kFull, tgt[0], cur & 31), t1 = __shfl_sync(kFull, tgt[1], cur & 31);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (lane + 32 * h < p.n_max) p.accept[at + lane + 32 * h] = mine[h];
+    if (lane == 0) {
+        p.n_accept[b] = count;
+        p.next[b] = cur < 0 ? first : cur < 32 ? t0 : t1;
+    }
+}
+
+// ---- rows into tail pages -----------------------------------------------------------------------------------------------------
+
+struct AppendParams {
+    const void *k_new[ENL_TAIL_LAYERS], *v_new[ENL_TAIL_LAYERS];
+    void *k_tail[ENL_TAIL_LAYERS], *v_tail[ENL_TAIL_LAYERS];
+    const int32_t *slot, *accept, *n_accept, *tail_len;
+    int32_t *tail_len_out;                                  // null: another launch of the call writes it
+    int32_t n_max, Hkv, D, n_slots;
+};
+
+// grid (requests x chunks of 64 rows, layers), eight warps that take a row each: 16-byte pieces, eight on their way a lane.  Bound by memory.
+constexpr int kAppendRows = 64, kAppendWarps = 8;
+__global__ void __launch_bounds__(kAppendWarps * 32) append_kernel(const __grid_constant__ AppendParams p)
+{
+    enl::pdl_trigger();
+    enl::pdl_wait();
+    const int chunks = (p.n_max + kAppendRows - 1) / kAppendRows;
+    const int b = static_cast<int>(blockIdx.x) / chunks, row0 = static_cast<int>(blockIdx.x) % chunks * kAppendRows;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int len = __ldcg(p.tail_len + b);
+    const int n = len < 0 ? 0 : p.n_accept ? max(0, min(__ldcg(p.n_accept + b), p.n_max)) : p.n_max;
+    const long long at = static_cast<long long>(b) * p.n_max;
+    // where row k comes from and goes to; false: it does not count
+    auto row_of = [&](int k, int &from, int &to) {
+        to = __ldcg(p.slot + at + k);
+        from = p.accept ? __ldcg(p.accept + at + k) : k;
+        return to >= 0 && to < p.n_slots && from >= 0 && from < p.n_max;
+    };
+    const int per_head = p.D / 8, pieces = p.Hkv * per_head;
+    const uint4 *ks = static_cast<const uint4 *>(p.k_new[blockIdx.y]), *vs = static_cast<const uint4 *>(p.v_new[blockIdx.y]);
+    uint4 *kd = static_cast<uint4 *>(p.k_tail[blockIdx.y]), *vd = static_cast<uint4 *>(p.v_tail[blockIdx.y]);
+    for (int k = row0 + warp; k < min(n, row0 + kAppendRows); k += kAppendWarps) {
+        int from, to;
+        if (!row_of(k, from, to)) continue;
+        const long long src = (at + from) * pieces;
+        const long long page = static_cast<long long>(to / kPageTokens) * p.Hkv;
+        auto place = [&](int c) { return ((page + c / per_head) * kPageTokens + to % kPageTokens) * per_head + c % per_head; };
+        for (int c0 = lane; c0 < pieces; c0 += 128) {
+            uint4 x[4], y[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c0 + 32 * u < pieces) {
+                    x[u] = __ldcg(ks + src + c0 + 32 * u);
+                    y[u] = __ldcg(vs + src + c0 + 32 * u);
+                }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c0 + 32 * u < pieces) {
+                    const long long d = place(c0 + 32 * u);
+                    kd[d] = x[u];
+                    vd[d] = y[u];
+                }
+        }
+    }
+    // the length, by the last warp of the first layer's first chunk (it changes no sign, which is all that the others read of it)
+    if (p.tail_len_out && blockIdx.y == 0 && row0 == 0 && warp == kAppendWarps - 1) {
+        int count = 0;
+        for (int k = lane; k < n; k += 32) {
+            int from, to;
+            count += row_of(k, from, to) ? 1 : 0;
+        }
+        for (int o = 16; o > 0; o >>= 1) count += __shfl_xor_sync(kFull, count, o);
+        if (lane == 0) p.tail_len_out[b] = len + count;
+    }
+}
+
+bool misaligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+int done(cudaError_t e)
+{
+    if (e == cudaSuccess) return ENL_OK;
+    cudaGetLastError();
+    return ENL_E_CUDA;
+}
+
+}  // namespace
+
+extern "C" int enl_tail_tables(const enl_tail_tables_args_t *a, void *cuda_stream)
+{
+    if (!a || !a->tail_len || !a->block_table || !a->n_blocks || !a->free_pages || !a->n_free || !a->slot) return ENL_E_INVAL;
+    if (a->batch < 1 || a->n_max < 1 || a->max_blocks < 1 || a->n_pages < 1) return ENL_E_INVAL;
+    for (const void *x : {static_cast<const void *>(a->tail_len), static_cast<const void *>(a->n_new), static_cast<const void *>(a->parent),
+                          static_cast<const void *>(a->pos_base), static_cast<const void *>(a->block_table), static_cast<const void *>(a->n_blocks),
+                          static_cast<const void *>(a->free_pages), static_cast<const void *>(a->n_free), static_cast<const void *>(a->slot),
+                          static_cast<const void *>(a->position), static_cast<const void *>(a->failed)})
+        if (misaligned(x, 4)) return ENL_E_INVAL;
+    if (misaligned(a->mask, 8)) return ENL_E_INVAL;
+    if (a->batch > ENL_TAIL_MAX_BATCH || a->n_max > ENL_TAIL_MAX_ROWS || a->max_blocks > kMaxPages || a->n_pages > kMaxPages) return ENL_E_LIMIT;
+    if ((a->parent || a->mask) && a->n_max > kMaxNodes) return ENL_E_LIMIT;
+    TablesParams p;
+    p.tail_len = a->tail_len;
+    p.n_new = a->n_new;
+    p.parent = a->parent;
+    p.pos_base = a->pos_base;
+    p.block_table = a->block_table;
+    p.n_blocks = a->n_blocks;
+    p.free_pages = a->free_pages;
+    p.n_free = a->n_free;
+    p.slot = a->slot;
+    p.position = a->position;
+    p.failed = a->failed;
+    p.mask = reinterpret_cast<unsigned long long *>(a->mask);
+    p.batch = a->batch;
+    p.n_max = a->n_max;
+    p.max_blocks = a->max_blocks;
+    p.n_pages = a->n_pages;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const int warps = a->batch * ((a->n_max + 63) / 64);
+    const bool one = warps <= kOneCtaWarps;
+    const int threads = 32 * std::max((a->batch + 31) / 32, one ? std::min(warps, 32) : 1);
+    const cudaError_t e = enl::launch_pdl_n(tables_kernel, dim3(1), dim3(threads), st, p, one ? 1 : 0);
+    if (e != cudaSuccess || one) return done(e);
+    return done(enl::launch_pdl(fill_kernel, dim3((warps + 7) / 8), dim3(256), 0, st, p));
+}
+
+extern "C" int enl_tree_accept(const enl_tree_accept_args_t *a, void *cuda_stream)
+{
+    if (!a || !a->token || !a->target || !a->accept || !a->n_accept || !a->next) return ENL_E_INVAL;
+    if (a->batch < 1 || a->n_max < 1) return ENL_E_INVAL;
+    for (const void *x : {static_cast<const void *>(a->n_new), static_cast<const void *>(a->parent), static_cast<const void *>(a->token),
+                          static_cast<const void *>(a->target), static_cast<const void *>(a->first), static_cast<const void *>(a->accept),
+                          static_cast<const void *>(a->n_accept), static_cast<const void *>(a->next)})
+        if (misaligned(x, 4)) return ENL_E_INVAL;
+    if (a->n_max > kMaxNodes) return ENL_E_LIMIT;
+    AcceptParams p;
+    p.n_new = a->n_new;
+    p.parent = a->parent;
+    p.token = a->token;
+    p.target = a->target;
+    p.first = a->first;
+    p.accept = a->accept;
+    p.n_accept = a->n_accept;
+    p.next = a->next;
+    p.batch = a->batch;
+    p.n_max = a->n_max;
+    const int warps = std::min(a->batch, 8);
+    return done(enl::launch_pdl(accept_kernel, dim3((a->batch + warps - 1) / warps), dim3(32 * warps), 0, static_cast<cudaStream_t>(cuda_stream), p));
+}
+
+extern "C" int enl_tail_append(const enl_tail_append_args_t *a, void *cuda_stream)
+{
+    if (!a || !a->k_new || !a->v_new || !a->k_tail || !a->v_tail || !a->slot || !a->tail_len || !a->tail_len_out) return ENL_E_INVAL;
+    if (a->n_layers < 1 || a->batch < 1 || a->n_max < 1 || a->n_kv_heads < 1 || a->head_dim < 8 || a->head_dim % 8 || a->n_pages < 1) return ENL_E_INVAL;
+    for (const void *x : {static_cast<const void *>(a->slot), static_cast<const void *>(a->accept), static_cast<const void *>(a->n_accept),
+                          static_cast<const void *>(a->tail_len), static_cast<const void *>(a->tail_len_out)})
+        if (misaligned(x, 4)) return ENL_E_INVAL;
+    for (int l = 0; l < a->n_layers; ++l) {
+        const void *four[4] = {a->k_new[l], a->v_new[l], a->k_tail[l], a->v_tail[l]};
+        for (const void *x : four)
+            if (!x || misaligned(x, 16)) return ENL_E_INVAL;
+    }
+    if (a->n_max > ENL_TAIL_MAX_ROWS || a->n_pages > kMaxPages) return ENL_E_LIMIT;
+    if (static_cast<int64_t>(a->n_kv_heads) * a->head_dim > (1 << 24)) return ENL_E_LIMIT;
+    const int64_t ctas = static_cast<int64_t>(a->batch) * ((a->n_max + kAppendRows - 1) / kAppendRows);
+    if (ctas > 0x7fffffff) return ENL_E_LIMIT;
+    AppendParams p;
+    p.slot = a->slot;
+    p.accept = a->accept;
+    p.n_accept = a->n_accept;
+    p.tail_len = a->tail_len;
+    p.n_max = a->n_max;
+    p.Hkv = a->n_kv_heads;
+    p.D = a->head_dim;
+    p.n_slots = a->n_pages * kPageTokens;
+    for (int l0 = 0; l0 < a->n_layers; l0 += ENL_TAIL_LAYERS) {
+        const int nl = std::min(ENL_TAIL_LAYERS, a->n_layers - l0);
+        for (int l = 0; l < ENL_TAIL_LAYERS; ++l) {
+            p.k_new[l] = l < nl ? a->k_new[l0 + l] : nullptr;
+            p.v_new[l] = l < nl ? a->v_new[l0 + l] : nullptr;
+            p.k_tail[l] = l < nl ? a->k_tail[l0 + l] : nullptr;
+            p.v_tail[l] = l < nl ? a->v_tail[l0 + l] : nullptr;
+        }
+        p.tail_len_out = l0 + nl == a->n_layers ? a->tail_len_out : nullptr;
+        const cudaError_t e = enl::launch_pdl(append_kernel, dim3(static_cast<unsigned>(ctas), nl), dim3(kAppendWarps * 32), 0,
+                                              static_cast<cudaStream_t>(cuda_stream), p);
+        if (e != cudaSuccess) return done(e);
+    }
+    return ENL_OK;
+}

@@ -21,11 +21,13 @@ ENL_DEVICE_NONE = -1
 ENL_REPLACE, ENL_APPEND = 0, 1
 ENL_PLAN_ONLY, ENL_MASS_ONLY = 1, 2
 ENL_OK, ENL_E_INVAL, ENL_E_NOGROUP, ENL_E_NOMEM, ENL_E_CUDA, ENL_E_TIMEOUT, ENL_E_LIMIT, ENL_E_EVICTED, ENL_E_CORRUPT = 0, -1, -2, -3, -4, -5, -6, -8, -9
+ENL_TREE_MAX_NODES, ENL_TAIL_MAX_BATCH, ENL_TAIL_MAX_ROWS, ENL_TAIL_LAYERS = 64, 1024, 16384, 64
 ENL_STATIC_MAX_SEGMENTS, ENL_STATIC_MAX_KEYS, ENL_STATIC_SCRATCH_BYTES = 255, 65536, 4 << 20
 
 EXPORTS = ("enl_cache_create", "enl_group_store", "enl_attend", "enl_cache_free", "enl_strerror",
            "enl_group_store_all_layers", "enl_group_len", "enl_cache_status", "enl_cache_selfcheck", "enl_plan_inspect", "enl_attend_static", "enl_static_status", "enl_cluster_assign",
-           "enl_cluster_assign_sums", "enl_select_knapsack", "enl_rope_rotate", "enl_tier_enable", "enl_group_evict", "enl_step_prepare", "enl_group_resident")
+           "enl_cluster_assign_sums", "enl_select_knapsack", "enl_rope_rotate", "enl_tier_enable", "enl_group_evict", "enl_step_prepare", "enl_group_resident",
+           "enl_tail_tables", "enl_attend_tree", "enl_tree_accept", "enl_tail_append")
 
 
 class CacheDesc(ctypes.Structure):
@@ -66,6 +68,28 @@ class PrepareStats(ctypes.Structure):
                 ("bytes_h2d", ctypes.c_int64), ("bytes_d2h", ctypes.c_int64)]
 
 
+class TailTablesArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_max", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("n_pages", ctypes.c_int32)] + \
+               [(n, ctypes.c_void_p) for n in ("tail_len", "n_new", "parent", "pos_base", "block_table", "n_blocks", "free_pages", "n_free", "slot",
+                                               "position", "mask", "failed")]
+
+
+class AttendTreeArgs(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_max", ctypes.c_int32), ("sel_ids", ctypes.c_void_p),
+                ("cu_sel", ctypes.c_void_p), ("n_sel", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("n_pages", ctypes.c_int32)] + \
+               [(n, ctypes.c_void_p) for n in ("tail_len", "n_new", "mask", "block_table", "q", "k_new", "v_new", "k_tail", "v_tail", "out")]
+
+
+class TreeAcceptArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_max", ctypes.c_int32)] + \
+               [(n, ctypes.c_void_p) for n in ("n_new", "parent", "token", "target", "first", "accept", "n_accept", "next")]
+
+
+class TailAppendArgs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_layers", "batch", "n_max", "n_kv_heads", "head_dim", "n_pages")] + \
+               [(n, ctypes.c_void_p) for n in ("k_new", "v_new", "k_tail", "v_tail", "slot", "accept", "n_accept", "tail_len", "tail_len_out")]
+
+
 class EnlError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: {strerror(code)} ({code})")
@@ -74,6 +98,7 @@ class EnlError(RuntimeError):
 
 _lib = None
 _native = None          # the _enl extension module
+_heads = {}             # cache handle -> (device, q heads, kv heads, head_dim): what the tensors of enl_attend_tree are checked against
 _n_layers = {}          # cache handle -> layer count (the all-layers store takes one pointer per layer)
 
 
@@ -131,6 +156,14 @@ def lib() -> ctypes.CDLL:
         L.enl_step_prepare.restype = ctypes.c_int
         L.enl_group_resident.argtypes = [ctypes.c_void_p, ctypes.c_int32]
         L.enl_group_resident.restype = ctypes.c_int
+        L.enl_tail_tables.argtypes = [ctypes.POINTER(TailTablesArgs), ctypes.c_void_p]
+        L.enl_tail_tables.restype = ctypes.c_int
+        L.enl_attend_tree.argtypes = [ctypes.c_void_p, ctypes.POINTER(AttendTreeArgs), ctypes.c_void_p]
+        L.enl_attend_tree.restype = ctypes.c_int
+        L.enl_tree_accept.argtypes = [ctypes.POINTER(TreeAcceptArgs), ctypes.c_void_p]
+        L.enl_tree_accept.restype = ctypes.c_int
+        L.enl_tail_append.argtypes = [ctypes.POINTER(TailAppendArgs), ctypes.c_void_p]
+        L.enl_tail_append.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -142,6 +175,8 @@ def _binding():
         lib()
         from . import _enl
         _enl.set_int32_converter(_i32)
+        import torch
+        _enl.set_dtypes(torch.bfloat16, torch.int32, torch.int64)
         _native = _enl
     return _native
 
@@ -173,6 +208,7 @@ def enl_cache_create(n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: i
     if rc != ENL_OK:
         raise EnlError(rc, "enl_cache_create")
     _n_layers[int(h.value)] = int(n_layers)
+    _heads[int(h.value)] = (int(device), int(n_q_heads), int(n_kv_heads), int(head_dim))
     return h.value
 
 
@@ -288,6 +324,59 @@ def enl_rope_rotate(rows, positions=None, first_pos: int = 0, base: float = 1000
         raise EnlError(rc, "enl_rope_rotate")
 
 
+def _on_device_of(t, call, *args) -> int:
+    """``call(device, *args)`` with the tensor's device as the current one (these calls have no cache that names it)."""
+    import torch
+    at = t.get_device()
+    if at < 0 or at == torch.cuda.current_device():
+        return call(at, *args)
+    with torch.cuda.device(at):
+        return call(at, *args)
+
+
+def enl_tail_tables(tail_len, block_table, n_blocks, free_pages, n_free, slots, positions=None, mask=None, n_new=None, parent=None,
+                    pos_base=None, failed=None, stream: int = 0) -> None:
+    """Room for the next rows of every request, and where they go.  Contiguous CUDA tensors, int32 but for ``mask`` (int64): ``tail_len``,
+    ``n_blocks``, ``n_new``, ``pos_base`` ``[B]``, ``block_table`` ``[B, max_blocks]``, ``free_pages`` ``[n_pages]``, ``n_free`` and ``failed``
+    ``[1]``, ``slots``, ``positions``, ``mask`` and ``parent`` ``[B, n_max]``.  ``block_table``, ``n_blocks``, ``free_pages`` and ``n_free`` are
+    updated, ``slots``, ``positions`` and ``mask`` are results."""
+    rc = _on_device_of(slots, (_native or _binding()).tail_tables, tail_len, block_table, n_blocks, free_pages, n_free, slots, positions, mask,
+                       n_new, parent, pos_base, failed, stream or None)
+    if rc != ENL_OK:
+        raise EnlError(rc, "enl_tail_tables")
+
+
+def enl_attend_tree(cache: int, layer: int, sel_ids: Sequence[int], q, k_new, v_new, k_tail, v_tail, block_table, tail_len, out, n_new=None,
+                    mask=None, cu_sel=None, stream: int = 0) -> None:
+    """The nodes of every request's tree over its selected groups, its tail and their ancestors.  Contiguous CUDA tensors: ``q`` and ``out``
+    ``[B, n_max, Hq, D]``, ``k_new`` and ``v_new`` ``[B, n_max, Hkv, D]``, ``k_tail`` and ``v_tail`` ``[n_pages, Hkv, 16, D]`` bf16, ``block_table``
+    ``[B, max_blocks]``, ``tail_len`` and ``n_new`` ``[B]`` int32, ``mask`` ``[B, n_max]`` int64 (None: a chain).  One token per request: ``n_max`` 1."""
+    native = _native or _binding()
+    device, n_q_heads, n_kv_heads, head_dim = _heads[cache]
+    rc = native.attend_tree(device, cache, layer, sel_ids, q, k_new, v_new, k_tail, v_tail, block_table, tail_len, out, n_new, mask, cu_sel,
+                            n_q_heads, n_kv_heads, head_dim, stream or None)
+    if rc != ENL_OK:
+        raise EnlError(rc, "enl_attend_tree")
+
+
+def enl_tree_accept(parent, token, target, accept, n_accept, next_token, n_new=None, first=None, stream: int = 0) -> None:
+    """Which drafted tokens the model would have written itself.  Contiguous int32 CUDA tensors: ``parent`` (None: a chain), ``token``, ``target``
+    and ``accept`` ``[B, n_max]``, the others ``[B]``; ``accept``, ``n_accept`` and ``next_token`` are results."""
+    rc = _on_device_of(token, (_native or _binding()).tree_accept, parent, token, target, accept, n_accept, next_token, n_new, first,
+                       stream or None)
+    if rc != ENL_OK:
+        raise EnlError(rc, "enl_tree_accept")
+
+
+def enl_tail_append(ks, vs, k_tails, v_tails, slots, tail_len, tail_len_out, accept=None, n_accept=None, stream: int = 0) -> None:
+    """Rows ``accept`` of every layer's ``ks`` and ``vs`` (``[B, n_max, Hkv, D]`` bf16, a contiguous CUDA tensor per layer) into its tail pages
+    (``[n_pages, Hkv, 16, D]``) at ``slots`` ``[B, n_max]``; ``tail_len_out`` = ``tail_len`` + rows appended (it may be the same tensor)."""
+    rc = _on_device_of(slots, (_native or _binding()).tail_append, ks, vs, k_tails, v_tails, slots, tail_len, tail_len_out, accept, n_accept,
+                       stream or None)
+    if rc != ENL_OK:
+        raise EnlError(rc, "enl_tail_append")
+
+
 def enl_tier_enable(cache: int, host_tokens: int) -> None:
     rc = lib().enl_tier_enable(cache, int(host_tokens))
     if rc != ENL_OK:
@@ -316,6 +405,7 @@ def enl_group_resident(cache: int, group_id: int) -> int:
 
 def enl_cache_free(cache: int) -> None:
     _n_layers.pop(int(cache), None)
+    _heads.pop(int(cache), None)
     lib().enl_cache_free(cache)
 
 
