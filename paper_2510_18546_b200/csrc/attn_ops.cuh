@@ -11,6 +11,11 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// several arrivals at once
+__device__ __forceinline__ void mbar_arrive_n(uint32_t bar, uint32_t n)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
+}
 // A test that never suspends (about 35 cycles until its result can be used, half of a poll with a suspend hint).
 __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
 {

@@ -202,11 +202,13 @@ struct TreeMergeParams {
     const int4 *part_head;
     void *out;
     int32_t n_max, Hq, Hkv, rep;
+    int32_t row_groups;     // groups of 32 rows (nodes x q heads of a kv head)
 };
 constexpr int kTreeMaxNodes = 64;   // bits of a mask
 cudaError_t prepare_tree(int head_dim);
 cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_t st);
-cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int row_tiles, int batch, cudaStream_t st);
+// deep: few units, whose streams have many splits
+cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, bool deep, cudaStream_t st);
 
 struct CombineParams {
     const float *part_o, *part_lse, *part_slot;

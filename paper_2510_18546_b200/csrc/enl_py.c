@@ -298,6 +298,25 @@ done:
     return ret;
 }
 
+/* What a tensor is made of, as the DLPack exchange interface of torch 2.10 and later tells it without a call into Python: five method calls
+ * a tensor are 0.3 us, 48 us of an append over 40 layers.  (Declared here as far as it is used: the interface is a fixed binary one, versions 1.x.) */
+typedef struct {
+    void *data;
+    struct { int32_t type, id; } device;
+    int32_t ndim;
+    struct { uint8_t code, bits; uint16_t lanes; } dtype;
+    int64_t *shape, *strides;
+    uint64_t byte_offset;
+} view_t;
+typedef struct {
+    struct { uint32_t major, minor; void *older; } header;
+    void *allocate, *to_managed, *from_managed;
+    int (*view)(void *tensor, view_t *out);
+} exchange_t;
+enum { kCuda = 2, kInt = 0, kBfloat = 4 };
+static PyTypeObject *t_tensor;                              /* torch.Tensor, whose exchange interface this is: */
+static const exchange_t *exchange;                          /* NULL: the methods are asked */
+
 /* A tensor whose type, number of dimensions, layout and device are checked (the lengths of these calls are device values: nothing behind the
  * binding could tell a tensor of another shape).  `dims` receives its shape; the first tensor of a call sets *device.  ValueError. */
 static int checked(PyObject *t, const char *name, PyObject *dtype, int ndim, int64_t *dims, void **ptr, long *device, int optional)
@@ -308,6 +327,23 @@ static int checked(PyObject *t, const char *name, PyObject *dtype, int ndim, int
         PyErr_Format(PyExc_ValueError, "%s is missing", name);
         return -1;
     }
+    view_t w;
+    if (exchange && Py_TYPE(t) == t_tensor && exchange->view(t, &w) == 0) {
+        int fine = w.device.type == kCuda && (*device == -2 || w.device.id == *device) && w.ndim == ndim && w.dtype.lanes == 1 &&
+                   (dtype == t_bf16 ? w.dtype.code == kBfloat && w.dtype.bits == 16 : w.dtype.code == kInt && w.dtype.bits == (dtype == t_int32 ? 32 : 64));
+        int64_t step = 1;
+        for (int i = ndim - 1; fine && i >= 0; --i) {
+            fine = w.shape[i] > 0 && (w.shape[i] == 1 || w.strides[i] == step);
+            step *= w.shape[i];
+            dims[i] = w.shape[i];
+        }
+        if (fine) {
+            *device = w.device.id;
+            *ptr = (char *)w.data + w.byte_offset;
+            return 0;
+        }                                                   /* else what is wrong is said below */
+    }
+    PyErr_Clear();
     PyObject *v = PyObject_GetAttr(t, s_dtype);
     if (!v) return -1;
     Py_DECREF(v);                                           /* torch keeps its dtypes */
@@ -587,12 +623,18 @@ done:
     return ret;
 }
 
-/* set_dtypes(bfloat16, int32, int64): torch's */
-static PyObject *py_set_dtypes(PyObject *self, PyObject *const *v, Py_ssize_t nargs)
+/* set_types(bfloat16, int32, int64, Tensor, exchange): torch's; exchange: the capsule of Tensor's DLPack exchange interface, or None */
+static PyObject *py_set_types(PyObject *self, PyObject *const *v, Py_ssize_t nargs)
 {
     (void)self;
-    if (want_args(nargs, 3)) return NULL;
-    for (int i = 0; i < 3; ++i) Py_INCREF(v[i]);
+    if (want_args(nargs, 5)) return NULL;
+    if (!PyType_Check(v[3])) { PyErr_SetString(PyExc_TypeError, "the tensor type"); return NULL; }
+    for (int i = 0; i < 4; ++i) Py_INCREF(v[i]);
+    if (PyCapsule_IsValid(v[4], "dlpack_exchange_api")) {
+        exchange = PyCapsule_GetPointer(v[4], "dlpack_exchange_api");
+        if (exchange && (exchange->header.major != 1 || !exchange->view)) exchange = NULL;
+    }
+    Py_XSETREF(t_tensor, (PyTypeObject *)v[3]);
     Py_XSETREF(t_bf16, v[0]);
     Py_XSETREF(t_int32, v[1]);
     Py_XSETREF(t_int64, v[2]);
@@ -617,7 +659,7 @@ static PyMethodDef methods[] = {
     {"attend_tree", (PyCFunction)(void (*)(void))py_attend_tree, METH_FASTCALL, NULL},
     {"tree_accept", (PyCFunction)(void (*)(void))py_tree_accept, METH_FASTCALL, NULL},
     {"tail_append", (PyCFunction)(void (*)(void))py_tail_append, METH_FASTCALL, NULL},
-    {"set_dtypes", (PyCFunction)(void (*)(void))py_set_dtypes, METH_FASTCALL, NULL},
+    {"set_types", (PyCFunction)(void (*)(void))py_set_types, METH_FASTCALL, NULL},
     {"set_int32_converter", py_set_converter, METH_O, NULL},
     {NULL, NULL, 0, NULL},
 };

@@ -169,7 +169,8 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         mp.Hq = d.n_q_heads;
         mp.Hkv = d.n_kv_heads;
         mp.rep = c->rep;
-        if (launch_tree_merge(mp, d.head_dim, row_tiles, B, st) != cudaSuccess) { cudaGetLastError(); return ENL_E_CUDA; }
+        mp.row_groups = ceil_div(a->n_max * c->rep, 32);
+        if (launch_tree_merge(mp, d.head_dim, B, grid > 4 * units, st) != cudaSuccess) { cudaGetLastError(); return ENL_E_CUDA; }
     }
     return ENL_OK;
 }

@@ -84,81 +84,103 @@ __device__ __forceinline__ Request request_of(const TreeParams &p, int b)
     }
     return r;
 }
-template <typename T>
-__device__ __forceinline__ T warp_sum(T x)
-{
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(kFull, x, o);
-    return x;
-}
 
+// Range s of ns of the steps.
+__device__ __forceinline__ void cut(Share &out, int steps, int s, int ns)
+{
+    const int each = steps / ns, more = steps - each * ns;
+    out.j_beg = each * s + min(s, more);
+    out.j_end = out.j_beg + each + (s < more ? 1 : 0);
+    out.n_splits = ns;
+}
 // The streams of all requests, kv heads and row tiles ("units") are cut into ranges of about `chunk` steps, as few steps as the grid has CTAs for.
-// CTA order: request, kv head, split, row tile (the tiles of a unit read the same keys at the same time).  By one warp; the first
-// CTA's leaves what the merge kernel has to know: per request the first CTA, its splits, row tiles and nodes.
-__device__ void find_share(const TreeParams &p, int lane, Share &out)
+// CTA order: request, kv head, split, row tile (the tiles of a unit read the same keys at the same time).  Every warp works it out for itself, so
+// that none waits for another (by one warp, with 64-bit arithmetic and a barrier behind it, 2.1 us of a launch, 3.7 for 16 requests).  With `heads`
+// the warp leaves what the merge kernel has to know: per request the first CTA, its splits, row tiles and nodes.
+__device__ __forceinline__ Share find_share(const TreeParams &p, int lane, bool heads)
 {
     const int grid = static_cast<int>(gridDim.x), idx = static_cast<int>(blockIdx.x);
-    Request r = request_of(p, lane);
-    long long work = 0, units = 0;
-    int longest = 0;
+    const Request r = request_of(p, p.batch == 1 ? 0 : lane);
+    Share out = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+    if (p.batch == 1) {
+        if (r.n == 0) {
+            if (heads && lane == 0) p.part_head[0] = make_int4(0, 0, 0, 0);
+            return out;
+        }
+        const int units = r.tiles * p.Hkv;
+        const int ns = p.may_split ? max(1, min(grid / units, r.steps / p.min_steps)) : 1;
+        if (heads && lane == 0) p.part_head[0] = make_int4(0, ns, r.tiles, r.n);
+        if (idx >= units * ns) return out;
+        const int above = idx / r.tiles;
+        out.kvh = above / ns;
+        out.rt = idx - above * r.tiles;
+        cut(out, r.steps, above - out.kvh * ns, ns);
+        out.n_entries = r.n_entries;
+        out.stream_off = r.stream_off;
+        out.len = r.len;
+        out.n = r.n;
+        return out;
+    }
+    float work = 0.f;
+    int units = 0, longest = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
         const Request q = b0 ? request_of(p, b0 + lane) : r;
-        work += static_cast<long long>(q.tiles) * p.Hkv * q.steps;
+        work += static_cast<float>(q.tiles * p.Hkv) * static_cast<float>(q.steps);
         units += q.tiles * p.Hkv;
         longest = max(longest, q.steps);
     }
-    work = warp_sum(work);
-    units = warp_sum(units);
+    for (int o = 16; o > 0; o >>= 1) work += __shfl_xor_sync(kFull, work, o);
+    units = __reduce_add_sync(kFull, units);
     longest = __reduce_max_sync(kFull, longest);
-    int chunk = longest;
+    // One over the steps of a range; every warp of the launch comes to the same one, and to the same number of splits of a request by it.
+    auto splits_of = [](int steps, float inv) { return static_cast<int>(ceilf(static_cast<float>(steps) * inv)); };
+    float chunk = static_cast<float>(max(longest, 1));
+    const float floor_steps = static_cast<float>(p.min_steps);
     if (p.may_split && units < grid && longest > p.min_steps) {
-        // enough for certain: sum of ceil(steps / chunk) <= work / chunk + units
-        const long long sure = (work + grid - units - 1) / (grid - units);
-        chunk = static_cast<int>(min(static_cast<long long>(longest), max(sure, static_cast<long long>(p.min_steps))));
+        // enough for certain: sum of ceil(steps / chunk) <= work / chunk + units (and a little for the rounding of the quotients)
+        const float sure = fminf(chunk, fmaxf(work * 1.001f / static_cast<float>(grid - units), floor_steps));
         if (p.batch <= 32) {
             // the shortest of 32 lengths that the grid has CTAs for, a lane each
-            const long long least = max((work + grid - 1) / grid, static_cast<long long>(p.min_steps));
-            const int mine = static_cast<int>(least) + static_cast<int>((chunk - least) * lane / 31);
-            if (chunk > least) {
-                long long ctas = 0;
-                for (int b = 0; b < p.batch; ++b) {
-                    const int steps = __shfl_sync(kFull, r.steps, b), tiles = __shfl_sync(kFull, r.tiles, b);
-                    ctas += static_cast<long long>((steps + mine - 1) / mine) * tiles * p.Hkv;
-                }
-                const unsigned fit = __ballot_sync(kFull, ctas <= grid);
-                if (fit) chunk = __shfl_sync(kFull, mine, __ffs(fit) - 1);
-            }
+            const float least = fminf(sure, fmaxf(work / static_cast<float>(grid), floor_steps));
+            const float mine = least + (sure - least) * (static_cast<float>(lane) / 31.f), inv = 1.f / mine;
+            int ctas = 0;
+            for (int b = 0; b < p.batch; ++b)
+                ctas += splits_of(__shfl_sync(kFull, r.steps, b), inv) * __shfl_sync(kFull, r.tiles, b);
+            const unsigned fit = __ballot_sync(kFull, ctas * p.Hkv <= grid);
+            chunk = __shfl_sync(kFull, lane == 31 ? sure : mine, fit ? __ffs(fit) - 1 : 31);
+        } else {
+            chunk = sure;
         }
     }
-    chunk = max(chunk, 1);
-    out.n_splits = 0;
+    const float inv = 1.f / chunk;
     int first = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
         const Request q = b0 ? request_of(p, b0 + lane) : r;
-        const int ns = (q.steps + chunk - 1) / chunk, mine = ns * q.tiles * p.Hkv;
+        const int ns = q.tiles ? max(1, splits_of(q.steps, inv)) : 0, mine = ns * q.tiles * p.Hkv;
         int upto = mine;
         for (int o = 1; o < 32; o <<= 1) {
             const int t = __shfl_up_sync(kFull, upto, o);
             if (lane >= o) upto += t;
         }
-        if (idx == 0 && p.part_head && b0 + lane < p.batch) p.part_head[b0 + lane] = make_int4(first + upto - mine, ns, q.tiles, q.n);
-        const int local = idx - (first + upto - mine);
-        if (local >= 0 && local < mine) {                             // (in one lane at most)
-            out.b = b0 + lane;
-            out.rt = local % q.tiles;
-            const int s = local / q.tiles % ns;
-            out.kvh = local / (q.tiles * ns);
-            out.n_splits = ns;
-            out.j_beg = static_cast<int>(static_cast<long long>(q.steps) * s / ns);
-            out.j_end = static_cast<int>(static_cast<long long>(q.steps) * (s + 1) / ns);
-            out.n_entries = q.n_entries;
-            out.stream_off = q.stream_off;
-            out.len = q.len;
-            out.n = q.n;
-        }
-        const bool found = __any_sync(kFull, local >= 0 && local < mine);
+        const int before = first + upto - mine;
+        if (heads && b0 + lane < p.batch) p.part_head[b0 + lane] = make_int4(before, ns, q.tiles, q.n);
+        const unsigned who = __ballot_sync(kFull, idx >= before && idx < before + mine);
         first += __shfl_sync(kFull, upto, 31);
-        if (found && (idx != 0 || !p.part_head)) break;
+        if (!who) continue;
+        const int from = __ffs(who) - 1;
+        const int local = idx - __shfl_sync(kFull, before, from), n_s = __shfl_sync(kFull, ns, from), tiles = __shfl_sync(kFull, q.tiles, from);
+        const int above = local / tiles;
+        out.b = b0 + from;
+        out.kvh = above / n_s;
+        out.rt = local - above * tiles;
+        cut(out, __shfl_sync(kFull, q.steps, from), above - out.kvh * n_s, n_s);
+        out.n_entries = __shfl_sync(kFull, q.n_entries, from);
+        out.stream_off = __shfl_sync(kFull, q.stream_off, from);
+        out.len = __shfl_sync(kFull, q.len, from);
+        out.n = __shfl_sync(kFull, q.n, from);
+        if (!heads) break;
     }
+    return out;
 }
 
 template <int D>
@@ -183,8 +205,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const __grid_constant
     auto bar_v_empty = [&](int x) { return bar0 + 8u * (7 + 3 * C::kRing + x); };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kBarOff + 8 * (7 + 4 * C::kRing));
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    Share *share = reinterpret_cast<Share *>(tmem_slot + 2);
-    static_assert(8 * (7 + 4 * C::kRing) + 8 + sizeof(Share) <= 384, "shared memory");
+    static_assert(8 * (7 + 4 * C::kRing) + 8 <= 384, "shared memory");
 
     // ---- set-up ----
     if (warp == kMmaWarp) {
@@ -192,39 +213,37 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const __grid_constant
                      ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    // Everything that says what to do (plan, lengths, block tables) may come from the kernel before.  The next one may start only after
-    // this wait: attention launches rely on it (see enl_attend).
-    pdl_wait();
-    pdl_trigger();
-    if (warp == 0) {
-        Share s;
-        find_share(p, lane, s);
-        const unsigned who = __ballot_sync(kFull, s.n_splits > 0);
-        if (who ? lane == __ffs(who) - 1 : lane == 0) {
-            *share = s;
-            *abort_flag = 0;
-            const int rows = s.n_splits > 0 ? min(kTileRows, s.n * p.rep - s.rt * kTileRows) : kTileRows;
-            mbar_init(bar_q_full, 1);
-            mbar_init(bar_pv_done, 1);
-            mbar_init(bar_o_done, 1);
-            for (int b = 0; b < 2; ++b) {
-                mbar_init(bar_s_full(b), 1);
-                mbar_init(bar_p_full(b), static_cast<uint32_t>((rows + 31) / 32));   // one arrival per softmax warp with rows
-            }
-            for (int x = 0; x < C::kRing; ++x) {
-                mbar_init(bar_k_full(x), 1);
-                mbar_init(bar_k_empty(x), 1);
-                mbar_init(bar_v_full(x), 1);
-                mbar_init(bar_v_empty(x), 1);
-            }
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (threadIdx.x == 0) {
+        *abort_flag = 0;
+        mbar_init(bar_q_full, 1);
+        mbar_init(bar_pv_done, 1);
+        mbar_init(bar_o_done, 1);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(bar_s_full(b), 1);
+            mbar_init(bar_p_full(b), kSoftmaxWarps);              // (the first warp arrives for those without rows, too)
         }
+        for (int x = 0; x < C::kRing; ++x) {
+            mbar_init(bar_k_full(x), 1);
+            mbar_init(bar_k_empty(x), 1);
+            mbar_init(bar_v_full(x), 1);
+            mbar_init(bar_v_empty(x), 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if ((warp == kKWarp || warp == kVWarp) && lane < 4) {
+        const CUtensorMap *tm = warp == kKWarp ? (lane == 0 ? &p.tm_kpool : lane == 1 ? &p.tm_ktail : lane == 2 ? &p.tm_knew : &p.tm_q)
+                                               : (lane == 0 ? &p.tm_vpool : lane == 1 ? &p.tm_vtail : &p.tm_vnew);
+        asm volatile("prefetch.tensormap [%0];" ::"l"(tm) : "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
-    const Share w = *share;
+    // Everything that says what to do (plan, lengths, block tables) may come from the kernel before.  The next one may start only after
+    // this wait: attention launches rely on it (see enl_attend).
+    pdl_wait();
+    pdl_trigger();
+    const Share w = find_share(p, lane, p.part_head && blockIdx.x == 0 && warp == kMmaWarp);
     const int n_steps = w.n_splits > 0 ? w.j_end - w.j_beg : 0;     // at least one where there is anything to do
     const int tail_pages = tail_pages_of(w.len);
     bool ok = true;
@@ -345,7 +364,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const __grid_constant
     } else if (n_steps > 0 && warp < kSoftmaxWarps && w.rt * kTileRows + warp * 32 < w.n * p.rep) {
         // ================= softmax: one thread per query row =================
         const int rep = p.rep, lr = 31 - __clz(rep);
-        const int r = warp * 32 + lane;
+        const int r = warp * 32 + lane, n_act = (min(kTileRows, w.n * rep - w.rt * kTileRows) + 31) >> 5;      // softmax warps with rows
         const int t = w.rt * (kTileRows >> lr) + (r >> lr);           // node
         const bool row_valid = t < w.n;
         const uint32_t lane_sel = static_cast<uint32_t>(warp * 32) << 16;
@@ -424,7 +443,9 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const __grid_constant
 
             // The reference moves only when the row maximum has grown by more than the threshold; then sum and accumulator are
             // rescaled, behind P V of the step before (the one before that was done when these scores were).
-            const bool need = m_cand > m + kRescaleThreshold;       // also true when m == -inf < m_cand
+            // (Rows of the tile that are no nodes hold whatever lay in shared memory: they must not move the others' references, or results
+            // would differ in their last bits from run to run.)
+            const bool need = row_valid && m_cand > m + kRescaleThreshold;       // also true when m == -inf < m_cand
             if (__any_sync(kFull, need)) {
                 const float m_new = fmaxf(m, m_cand);
                 const float alpha = (m_new == kNegInf) ? 1.f : ex2(m - m_new);
@@ -489,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const __grid_constant
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar_p_full(b));
+            if (lane == 0) mbar_arrive_n(bar_p_full(b), warp == 0 ? static_cast<uint32_t>(kSoftmaxWarps + 1 - n_act) : 1u);
             float lo0, hi0, lo1, hi1;
             unpack2(ps2[0], lo0, hi0);
             unpack2(ps2[1], lo1, hi1);
@@ -534,85 +555,89 @@ __global__ void __launch_bounds__(kThreads, 2) tree_kernel(const __grid_constant
     }
 }
 
-// Puts the splits of a row together: out = sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  grid (channels / 8, kv heads x row tiles, requests); a
-// thread takes eight channels of a row and every kGroups-th split, the groups are added up in shared memory.
-constexpr int kMergeThreads = 512;
-template <int D>
-__global__ void __launch_bounds__(kMergeThreads) tree_merge_kernel(const __grid_constant__ TreeMergeParams p)
+// Puts the splits of a row together: out = sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M), in the order of the splits.  A CTA takes 32 rows of a
+// unit, a lane each; grid.x runs over units and groups of 32 rows, grid.y over channels.  Few registers and little shared memory: its
+// CTAs find a place beside those of the attention kernel and wait there for its end (with 512 threads of 64 registers they started
+// after it: 4.7 us behind it for one token of 8 kv heads, ...).
+//   kDeep: four channels a CTA; its warps take every fourth split, six of them at a time, and are added up in shared memory
+//   else (calls with many units, whose streams have few splits): sixteen channels a CTA, four a warp, which takes all splits
+constexpr int kMergeWarps = 4;
+template <int D, bool kDeep>
+__global__ void __launch_bounds__(kMergeWarps * 32, 8) tree_merge_kernel(const __grid_constant__ TreeMergeParams p)
 {
-    __shared__ float sums[kMergeThreads][9];
-    __shared__ float refs[kMergeThreads];
+    __shared__ float4 sums[kMergeWarps][32];
+    __shared__ float2 refs[kMergeWarps][32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int lr = 31 - __clz(p.rep);
+    const int row_groups = p.row_groups, b = static_cast<int>(blockIdx.x) / (p.Hkv * row_groups), at = static_cast<int>(blockIdx.x) - b * (p.Hkv * row_groups);
+    const int kvh = at / row_groups, rows0 = (at - kvh * row_groups) * 32, tile = rows0 / kTileRows;
+    const int quad = kDeep ? static_cast<int>(blockIdx.y) : static_cast<int>(blockIdx.y) * kMergeWarps + warp;
     pdl_trigger();
     pdl_wait();                                             // the partial results come from the previous kernel
-    const int b = blockIdx.z;
     const int4 head = __ldcg(p.part_head + b);              // first CTA, splits, row tiles, nodes
-    const int tile = static_cast<int>(blockIdx.y) / p.Hkv, kvh = static_cast<int>(blockIdx.y) % p.Hkv;
-    if (head.y < 2 || tile >= head.z) return;
-    const int lr = 31 - __clz(p.rep);
-    const int rows = min(kTileRows, (head.w << lr) - tile * kTileRows);
-    const int width = (rows + 31) & ~31, groups = kMergeThreads / width;
-    const int r = static_cast<int>(threadIdx.x) % width, g = static_cast<int>(threadIdx.x) / width;
-    const bool on = r < rows && g < groups;
-    float acc[8] = {}, m = kNegInf, l = 0.f;
-    if (on) {
-        constexpr int kAhead = 4;                           // splits on their way at once
-        for (int s0 = g; s0 < head.y; s0 += kAhead * groups) {
-            float lse[kAhead];
-            float4 x[kAhead][2];
+    const int row = rows0 + lane;
+    if (head.y < 2 || rows0 >= head.w << lr) return;
+    const bool on = row < head.w << lr;
+    const int r = row % kTileRows;
+    const long long cta0 = head.x + static_cast<long long>(kvh) * head.y * head.z + tile;
+    constexpr int kAhead = kDeep ? 6 : 4, kEvery = kDeep ? kMergeWarps : 1;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = kNegInf, l = 0.f;
+    for (int s0 = kDeep ? warp : 0; s0 < head.y && on; s0 += kAhead * kEvery) {
+        float lse[kAhead];
+        float4 x[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int s = s0 + u * groups;
-                lse[u] = kNegInf;
-                if (s < head.y) {
-                    const long long cta = head.x + (static_cast<long long>(kvh) * head.y + s) * head.z + tile;
-                    const float4 *o = reinterpret_cast<const float4 *>(p.part_o) + (cta * (D / 4) + blockIdx.x * 2) * kTileRows + r;
-                    lse[u] = __ldcg(p.part_lse + cta * kTileRows + r);
-                    x[u][0] = __ldcg(o);
-                    x[u][1] = __ldcg(o + kTileRows);
-                }
+        for (int u = 0; u < kAhead; ++u) {
+            const int s = s0 + u * kEvery;
+            lse[u] = kNegInf;
+            if (s < head.y) {
+                const long long cta = cta0 + static_cast<long long>(s) * head.z;
+                lse[u] = __ldcg(p.part_lse + cta * kTileRows + r);
+                x[u] = __ldcg(reinterpret_cast<const float4 *>(p.part_o) + (cta * (D / 4) + quad) * kTileRows + r);
             }
-            float m_new = m;
+        }
+        float m_new = m;
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) m_new = fmaxf(m_new, lse[u]);
-            if (m_new == kNegInf) continue;                 // splits that saw no key
-            const float alpha = ex2(m - m_new);
-            l *= alpha;
+        for (int u = 0; u < kAhead; ++u) m_new = fmaxf(m_new, lse[u]);
+        if (m_new == kNegInf) continue;                     // splits that saw no key
+        const float alpha = ex2(m - m_new);
+        l *= alpha;
+        acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+        m = m_new;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) acc[c] *= alpha;
-            m = m_new;
-#pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                if (lse[u] == kNegInf) continue;
-                const float f = ex2(lse[u] - m);
-                l += f;
-                acc[0] = fmaf(f, x[u][0].x, acc[0]); acc[1] = fmaf(f, x[u][0].y, acc[1]);
-                acc[2] = fmaf(f, x[u][0].z, acc[2]); acc[3] = fmaf(f, x[u][0].w, acc[3]);
-                acc[4] = fmaf(f, x[u][1].x, acc[4]); acc[5] = fmaf(f, x[u][1].y, acc[5]);
-                acc[6] = fmaf(f, x[u][1].z, acc[6]); acc[7] = fmaf(f, x[u][1].w, acc[7]);
-            }
+        for (int u = 0; u < kAhead; ++u) {
+            if (lse[u] == kNegInf) continue;
+            const float f = ex2(lse[u] - m);
+            l += f;
+            acc.x = fmaf(f, x[u].x, acc.x); acc.y = fmaf(f, x[u].y, acc.y);
+            acc.z = fmaf(f, x[u].z, acc.z); acc.w = fmaf(f, x[u].w, acc.w);
         }
     }
-    refs[threadIdx.x] = m;
+    if (kDeep) {
+        sums[warp][lane] = acc;
+        refs[warp][lane] = make_float2(m, l);
+        __syncthreads();
+        if (warp != 0) return;
+        float top = kNegInf;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) sums[threadIdx.x][c] = acc[c];
-    sums[threadIdx.x][8] = l;
-    __syncthreads();
-    if (g != 0 || r >= rows) return;
-    float top = m;
-    for (int k = 1; k < groups; ++k) top = fmaxf(top, refs[k * width + r]);
-    float total[9] = {};
-    if (top != kNegInf)
-        for (int k = 0; k < groups; ++k) {
-            const float f = ex2(refs[k * width + r] - top);
+        for (int g = 0; g < kMergeWarps; ++g) top = fmaxf(top, refs[g][lane].x);
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        l = 0.f;
 #pragma unroll
-            for (int c = 0; c < 9; ++c) total[c] = fmaf(f, sums[k * width + r][c], total[c]);
+        for (int g = 0; g < kMergeWarps; ++g) {
+            const float2 ml = refs[g][lane];
+            if (ml.x == kNegInf) continue;
+            const float f = ex2(ml.x - top);
+            const float4 x = sums[g][lane];
+            l = fmaf(f, ml.y, l);
+            acc.x = fmaf(f, x.x, acc.x); acc.y = fmaf(f, x.y, acc.y); acc.z = fmaf(f, x.z, acc.z); acc.w = fmaf(f, x.w, acc.w);
         }
-    const float inv = total[8] > 0.f ? 1.f / total[8] : 0.f;
-    const int t = tile * (kTileRows >> lr) + (r >> lr);
-    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
-                 ((static_cast<long long>(b) * p.n_max + t) * p.Hq + kvh * p.rep + (r & (p.rep - 1))) * D + blockIdx.x * 8);
-    *dst = make_uint4(pack_bf16(total[0] * inv, total[1] * inv), pack_bf16(total[2] * inv, total[3] * inv),
-                      pack_bf16(total[4] * inv, total[5] * inv), pack_bf16(total[6] * inv, total[7] * inv));
+    }
+    if (!on) return;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    uint2 *dst = reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) +
+                 ((static_cast<long long>(b) * p.n_max + (row >> lr)) * p.Hq + kvh * p.rep + (row & (p.rep - 1))) * D + quad * 4);
+    *dst = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
 }
 
 }  // namespace
@@ -633,13 +658,13 @@ cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int row_tiles, int batch, cudaStream_t st)
+cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, bool deep, cudaStream_t st)
 {
-    const dim3 grid(head_dim / 8, p.Hkv * row_tiles, batch);
-    cudaError_t e;
-    if (head_dim == 128) e = launch_pdl(tree_merge_kernel<128>, grid, dim3(kMergeThreads), 0, st, p);
-    else if (head_dim == 64) e = launch_pdl(tree_merge_kernel<64>, grid, dim3(kMergeThreads), 0, st, p);
-    else return cudaErrorInvalidValue;
+    if (head_dim != 128 && head_dim != 64) return cudaErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(batch) * p.Hkv * p.row_groups, deep ? head_dim / 4 : head_dim / (4 * kMergeWarps)), block(kMergeWarps * 32);
+    const auto kernel = head_dim == 128 ? (deep ? tree_merge_kernel<128, true> : tree_merge_kernel<128, false>)
+                                        : (deep ? tree_merge_kernel<64, true> : tree_merge_kernel<64, false>);
+    const cudaError_t e = launch_pdl(kernel, grid, block, 0, st, p);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -176,7 +176,7 @@ def _binding():
         from . import _enl
         _enl.set_int32_converter(_i32)
         import torch
-        _enl.set_dtypes(torch.bfloat16, torch.int32, torch.int64)
+        _enl.set_types(torch.bfloat16, torch.int32, torch.int64, torch.Tensor, getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))
         _native = _enl
     return _native
 
