@@ -168,7 +168,12 @@ struct StaticDecodeParams {
     int32_t page_off[kStaticMaxSeg + 2];    // the same in pages (16 keys of one slot, the last one of a slot partly filled)
 };
 
-// Drafted trees over selected groups and a growing tail (see enl_tree_sm100.cu)
+// Drafted trees over selected groups and a growing tail (see enl_tree_sm100.cu): one CTA of a call with several requests
+struct TreeItem {
+    int32_t head;           // request << 16 | kv head
+    int32_t part;           // tile of rows << 24 | split << 12 | splits
+    int32_t first, count;   // stream entries (cached pages) of the split
+};
 struct TreeParams {
     CUtensorMap tm_q;       // [batch * n_max][Hq][D]   box {64, rep, box_tokens}
     CUtensorMap tm_knew;    // as in AttnParams, the requests' nodes
@@ -177,8 +182,7 @@ struct TreeParams {
     CUtensorMap tm_vpool;
     CUtensorMap tm_ktail;   // the caller's tail pages, of the same format
     CUtensorMap tm_vtail;
-    EpInfo ep0;             // request 0 (used when the call has one)
-    const EpInfo *eps;
+    const TreeItem *items;  // (a single request's CTAs know their places from n_splits and n_entries)
     const int32_t *stream_page;
     const int32_t *stream_meta;
     const int32_t *block_table;     // [batch][max_blocks] pages of the tails
@@ -188,20 +192,23 @@ struct TreeParams {
     void   *out;            // bf16 [batch][n_max][Hq][D]
     float  *part_o;         // [CTA][D / 4][128 rows][4] outputs of splits, normalised by their own sums
     float  *part_lse;       // [CTA][128] their log2-sum-exps
-    int4   *part_head;      // [batch] first CTA, splits, row tiles, nodes (null when the call is not split)
     int32_t *status;        // as in AttnParams
     int32_t batch, n_max, max_blocks, n_tail_pages;
     int32_t Hq, Hkv, rep;
+    int32_t row_tiles;      // tiles of rows per kv head
     int32_t box_tokens;     // tokens of a Q box
-    int32_t may_split;
-    int32_t min_steps;      // a split takes as many steps of 64 keys, at least
+    int32_t n_splits, n_entries;    // of a single request
+    int32_t wait_first;     // as in AttnParams
     float   scale_log2;
 };
 struct TreeMergeParams {
     const float *part_o, *part_lse;
-    const int4 *part_head;
+    const int2 *heads;      // [batch] first CTA and splits of every request, or null: one request, n_splits
+    const int32_t *tail_len, *n_new;        // as in TreeParams
     void *out;
+    int32_t n_splits;
     int32_t n_max, Hq, Hkv, rep;
+    int32_t row_tiles;
     int32_t row_groups;     // groups of 32 rows (nodes x q heads of a kv head)
 };
 constexpr int kTreeMaxNodes = 64;   // bits of a mask

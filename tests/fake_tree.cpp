@@ -2,11 +2,11 @@
 #include "fake_runtime.cpp"
 
 namespace {
-int g_grid, g_may_split, g_box, g_deep;
+int g_grid, g_splits, g_box, g_deep;
 }
 extern "C" {
 int fake_grid() { return g_grid; }
-int fake_may_split() { return g_may_split; }
+int fake_splits() { return g_splits; }
 int fake_box() { return g_box; }
 int fake_deep() { return g_deep; }
 }
@@ -15,9 +15,9 @@ cudaError_t prepare_tree(int) { return g_fail_kind == 'P' ? cudaErrorInvalidValu
 cudaError_t launch_tree(const TreeParams &p, int, int grid, cudaStream_t)
 {
     g_grid = grid;
-    g_may_split = p.may_split;
+    g_splits = p.n_splits;
     g_box = p.box_tokens;
-    return note('t', 1);
+    return note('t', p.wait_first);
 }
 cudaError_t launch_tree_merge(const TreeMergeParams &, int, int, bool deep, cudaStream_t)
 {

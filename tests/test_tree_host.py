@@ -136,7 +136,9 @@ def test_plan_is_sent_once_and_again_when_something_changed(host):
     for layer in (0, 1, 1, 0):
         assert c.call(layer=layer) == enl.ENL_OK
     assert c.kinds() == "tu" * 4
-    assert c.call(n_max=7, max_blocks=40) == enl.ENL_OK and c.kinds() == "tu"      # device lengths and shapes are no part of it
+    assert c.call(n_new=None, mask=None, n_pages=50) == enl.ENL_OK and c.kinds() == "tu"
+    assert c.call(n_max=7) == enl.ENL_OK and c.call(max_blocks=40) == enl.ENL_OK and c.kinds() == "wtuwtu"    # what the splits go by
+    assert c.call() == enl.ENL_OK and c.kinds() == "wtu"
     assert c.call(sel=(2, 1, 0)) == enl.ENL_OK and c.kinds() == "wtu"
     c.store(1, 0)
     c.kinds()
@@ -160,13 +162,17 @@ def test_plans_of_the_two_attentions_are_kept_apart(host):
 
 
 def test_the_next_attention_need_not_wait_first(host):
-    """The kernel waits for what came before and holds its successors back until then, so an attend behind it may read the pool early."""
+    """Either attention leaves plan and pool behind as later ones may find them before the kernel before them has ended."""
     c = Host(host)
     assert c.attend() == enl.ENL_OK and host.fake_wait_first(1) == 1
     host.fake_clear()
     assert c.attend() == enl.ENL_OK and host.fake_wait_first(0) == 0
     c.store(3, 0)
-    assert c.call(sel=(0, 1)) == enl.ENL_OK
+    c.kinds()
+    for first in (1, 0, 0):
+        assert c.call(sel=(0, 1)) == enl.ENL_OK
+        at = host.fake_launches() - 2
+        assert host.fake_kind(at) == ord("t") and host.fake_wait_first(at) == first
     host.fake_clear()
     assert c.attend() == enl.ENL_OK                               # the plan is written anew: it waits
     assert host.fake_kind(0) == ord("w") and host.fake_wait_first(1) == 1
@@ -205,19 +211,25 @@ def test_plan_larger_than_its_buffers(host):
 
 
 def test_grid_and_splits(host):
-    """Two CTAs per multiprocessor and splits where the scratch buffer has room for them; else a CTA per unit."""
+    """Splits until two CTAs per multiprocessor have work, as few as come to the same number of steps, and none where scratch buffer or stream
+    are too short for them."""
     c = Host(host)
+    # 9 cached pages, a table of 32, one page of nodes: 42; a step of four pages each
     assert c.call() == enl.ENL_OK
-    assert (host.fake_grid(), host.fake_may_split(), host.fake_box()) == (296, 1, 16)
-    assert c.call(n_max=64) == enl.ENL_OK and (host.fake_grid(), host.fake_box()) == (296, 32)
-    assert c.call(sel=(), max_blocks=1, n_max=1) == enl.ENL_OK and (host.fake_grid(), host.fake_may_split()) == (8, 0)     # nothing to split
-    c = Host(host, scratch_bytes=100000)
-    assert c.call() == enl.ENL_OK and (host.fake_grid(), host.fake_may_split()) == (8, 0)
+    assert (host.fake_grid(), host.fake_splits(), host.fake_box()) == (8 * 11, 11, 16) and host.fake_deep() == 1
+    # 64 nodes are two tiles of rows, and four pages themselves
+    assert c.call(n_max=64) == enl.ENL_OK and (host.fake_grid(), host.fake_splits(), host.fake_box()) == (8 * 2 * 12, 12, 32)
     c.kinds()
-    assert c.call() == enl.ENL_OK and c.kinds() == "t"
+    assert c.call(sel=(), max_blocks=1, n_max=1) == enl.ENL_OK and (host.fake_grid(), host.fake_splits()) == (8, 1) and c.kinds() == "t"        # an empty plan
+    c = Host(host, scratch_bytes=100000)
+    assert c.call() == enl.ENL_OK and (host.fake_grid(), host.fake_splits()) == (8, 1)
     slot = 128 * 129 * 4
-    c = Host(host, scratch_bytes=256 + 20 * slot)
-    assert c.call() == enl.ENL_OK and (host.fake_grid(), host.fake_may_split()) == (20, 1)
+    c = Host(host, scratch_bytes=24 * slot)
+    assert c.call() == enl.ENL_OK and (host.fake_grid(), host.fake_splits()) == (24, 3) and host.fake_deep() == 0
+    # two requests: the longer one is cut into more
+    c = Host(host)
+    assert c.call(sel=(0, 1, 2, 3), batch=2, cu_sel=np.array([0, 0, 4], np.int32)) == enl.ENL_OK
+    assert host.fake_grid() <= 296 and host.fake_grid() % 8 == 0 and host.fake_splits() > 4
 
 
 # ---- the calls without a cache: nothing is followed before everything has been looked at ---------------------------------------
