@@ -151,9 +151,9 @@ struct enl_cache {
     bool plan_park = false;                 // every CTA walks few slots: it parks their sums in shared memory and writes the masses itself
     bool plan_finish = false;               // else a kernel behind the attention kernel turns log-sums into masses
     std::vector<int32_t> key_obj;           // object spans the row -> object map was built from
-    bool plan_tree = false;                 // the plan is for enl_attend_tree: streams, and a list of CTAs where there are several requests
+    bool plan_tree = false;                 // the plan is for enl_attend_tree: streams, and the CTAs' shares where there are several requests
     int32_t tree_rows = 0, tree_blocks = 0, tree_entries = 0;      // ... for this n_max and max_blocks; cached pages of a single request
-    std::vector<int32_t> tree_splits;       // working space of such a call
+    int32_t tree_slots = 0;                 // partial results per tile of rows
     bool tree_ready = false;                // the kernel of enl_attend_tree has been opted in
     bool plan_decode = false;               // the plan is for the one-token decode kernel
     int32_t plan_small_blocks = 0;          // > 0: the plan is for the kernel of short calls, with this many row blocks per kv head

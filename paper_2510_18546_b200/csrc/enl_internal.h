@@ -168,11 +168,13 @@ struct StaticDecodeParams {
     int32_t page_off[kStaticMaxSeg + 2];    // the same in pages (16 keys of one slot, the last one of a slot partly filled)
 };
 
-// Drafted trees over selected groups and a growing tail (see enl_tree_sm100.cu): one CTA of a call with several requests
-struct TreeItem {
+// Drafted trees over selected groups and a growing tail (see enl_tree_sm100.cu): a part of a unit, the stream of a request and kv head
+struct TreeSegment {
     int32_t head;           // request << 16 | kv head
-    int32_t part;           // tile of rows << 24 | split << 12 | splits
-    int32_t first, count;   // stream entries (cached pages) of the split
+    int32_t slot;           // of the partial results, -1: the part is the whole
+    int32_t first, count;   // stream entries (cached pages)
+    int32_t from, to, whole;// the part of the tail: from / whole to to / whole
+    int32_t pad;
 };
 struct TreeParams {
     CUtensorMap tm_q;       // [batch * n_max][Hq][D]   box {64, rep, box_tokens}
@@ -182,7 +184,8 @@ struct TreeParams {
     CUtensorMap tm_vpool;
     CUtensorMap tm_ktail;   // the caller's tail pages, of the same format
     CUtensorMap tm_vtail;
-    const TreeItem *items;  // (a single request's CTAs know their places from n_splits and n_entries)
+    const TreeSegment *segments;    // those of group i (the CTAs of its row_tiles tiles): segment_off[i] .. segment_off[i + 1] - 1
+    const int32_t *segment_off;     // (a single request's CTAs know their parts from n_splits and n_entries)
     const int32_t *stream_page;
     const int32_t *stream_meta;
     const int32_t *block_table;     // [batch][max_blocks] pages of the tails
@@ -190,8 +193,8 @@ struct TreeParams {
     const int32_t *n_new;           // [batch] nodes, or null: n_max
     const unsigned long long *mask; // [batch][n_max] nodes that a node sees (a bit each), or null: a chain
     void   *out;            // bf16 [batch][n_max][Hq][D]
-    float  *part_o;         // [CTA][D / 4][128 rows][4] outputs of splits, normalised by their own sums
-    float  *part_lse;       // [CTA][128] their log2-sum-exps
+    float  *part_o;         // [slot][row tile][D / 4][128 rows][4] outputs of parts, normalised by their own sums
+    float  *part_lse;       // [slot][row tile][128] their log2-sum-exps
     int32_t *status;        // as in AttnParams
     int32_t batch, n_max, max_blocks, n_tail_pages;
     int32_t Hq, Hkv, rep;
@@ -203,19 +206,19 @@ struct TreeParams {
 };
 struct TreeMergeParams {
     const float *part_o, *part_lse;
-    const int2 *heads;      // [batch] first CTA and splits of every request, or null: one request, n_splits
+    const int2 *heads;      // [request][kv head] first slot and parts of every unit, or null: one request, n_splits
     const int32_t *tail_len, *n_new;        // as in TreeParams
     void *out;
     int32_t n_splits;
     int32_t n_max, Hq, Hkv, rep;
     int32_t row_tiles;
-    int32_t row_groups;     // groups of 32 rows (nodes x q heads of a kv head)
+    int32_t row_groups;     // (filled in by the launcher)
 };
 constexpr int kTreeMaxNodes = 64;   // bits of a mask
 cudaError_t prepare_tree(int head_dim);
 cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_t st);
-// deep: few units, whose streams have many splits
-cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, bool deep, cudaStream_t st);
+// most: parts of the unit that has most
+cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, int most, cudaStream_t st);
 
 struct CombineParams {
     const float *part_o, *part_lse, *part_slot;

@@ -1,6 +1,8 @@
 // Host side of enl_attend_tree: checks, the gather plan of the selected groups, the launch of the kernels in enl_tree_sm100.cu.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <vector>
 
 #include "enl_cache.h"
 
@@ -8,17 +10,81 @@ using namespace enl;
 
 namespace {
 
-// How many splits a request's stream of `pages` pages gets that may have `most`: the fewest that come to as few steps (of four pages) per CTA as
-// `most` would, and none where that does not save what putting splits together costs, some four steps.
-int splits_for(int64_t pages, int64_t most)
+constexpr int kStepPages = kStepKeys / kPageTokens;
+constexpr int kMergeSteps = 4;      // what putting parts together costs, in steps of a CTA
+constexpr int kSegmentSteps = 2;    // what another segment of a CTA costs
+
+int64_t steps_of(int64_t pages) { return (pages + kStepPages - 1) / kStepPages; }
+
+// How many equal parts a stream of `pages` pages gets that may have `most`: the fewest that come to as few steps per CTA as `most` would, and
+// one where that does not save what putting them together costs.
+int64_t parts_for(int64_t pages, int64_t most)
 {
-    constexpr int kStepPages = kStepKeys / kPageTokens, kMergeSteps = 4;
-    auto steps_of = [&](int64_t ns) { return ((pages + ns - 1) / ns + kStepPages - 1) / kStepPages; };
-    most = std::max<int64_t>(1, std::min(most, (pages + kStepPages - 1) / kStepPages));
-    const int64_t steps = steps_of(most);
-    if (steps_of(1) <= steps + kMergeSteps) return 1;
-    return static_cast<int>((pages + steps * kStepPages - 1) / (steps * kStepPages));
+    most = std::max<int64_t>(1, std::min(most, steps_of(pages)));
+    const int64_t steps = steps_of((pages + most - 1) / most);
+    if (steps_of(pages) <= steps + kMergeSteps) return 1;
+    return (pages + steps * kStepPages - 1) / (steps * kStepPages);
 }
+
+// What the CTAs of a call of several requests do, made for streams of `pages[b]` pages (each of them `heads` times) and `groups` places for CTAs:
+// segments in the order of requests and kv heads, with steps as their unit, and where every group's segments begin.
+struct Shares {
+    std::vector<TreeSegment> segments;
+    std::vector<int32_t> off;
+    std::vector<int2> units;        // first slot and parts
+    int most = 1;                   // parts of the unit that has most
+    int32_t slots = 0;
+
+    void add(int b, int h, int64_t from, int64_t to, int64_t whole)
+    {
+        const int u = b * heads + h;
+        if (from == 0) units[u] = make_int2(slots, 0);
+        const bool all = from == 0 && to == whole;
+        segments.push_back(TreeSegment{b << 16 | h, all ? -1 : slots, 0, 0, static_cast<int32_t>(from), static_cast<int32_t>(to), static_cast<int32_t>(whole), 0});
+        if (!all) ++slots;
+        most = std::max(most, ++units[u].y);
+    }
+    // Equal parts of a request's streams, a CTA each: `parts[b]` of them.
+    void equal(const std::vector<int64_t> &parts)
+    {
+        for (size_t b = 0; b < parts.size(); ++b)
+            for (int h = 0; h < heads; ++h)
+                for (int64_t s = 0; s < parts[b]; ++s) {
+                    off.push_back(static_cast<int32_t>(segments.size()));
+                    add(static_cast<int>(b), h, s, s + 1, parts[b]);
+                }
+        off.push_back(static_cast<int32_t>(segments.size()));
+    }
+    // Runs of as many steps for every CTA, across units.  A run does not begin or end less than kSegmentSteps from a unit's own ends.
+    void runs(const std::vector<int64_t> &steps, int64_t groups)
+    {
+        int64_t total = 0, at = 0, cut = 0, j = 0;         // steps of all units, before this unit, where run j ends
+        for (int64_t s : steps) total += s * heads;
+        off.push_back(0);
+        for (size_t b = 0; b < steps.size(); ++b)
+            for (int h = 0; h < heads; ++h) {
+                const int64_t whole = steps[b];
+                int64_t from = 0;
+                for (;;) {
+                    cut = total * (j + 1) / groups - at;   // within this unit
+                    if (cut < from + kSegmentSteps && from > 0) cut = from;
+                    if (cut < kSegmentSteps) cut = 0;
+                    if (cut > whole - kSegmentSteps && cut < whole + kSegmentSteps) cut = whole;
+                    const int64_t to = std::min(cut, whole);
+                    if (to > from) add(static_cast<int>(b), h, from, to, whole);
+                    from = std::max(from, to);
+                    if (cut > whole || j + 1 >= groups) break;         // the run goes on in the next unit
+                    if (off.back() != static_cast<int32_t>(segments.size())) off.push_back(static_cast<int32_t>(segments.size()));
+                    ++j;
+                    if (cut >= whole) break;
+                }
+                if (from < whole) add(static_cast<int>(b), h, from, whole, whole);
+                at += whole;
+            }
+        if (off.back() != static_cast<int32_t>(segments.size())) off.push_back(static_cast<int32_t>(segments.size()));
+    }
+    int heads = 1;
+};
 
 }  // namespace
 
@@ -49,8 +115,7 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         static_cast<int64_t>(B) * a->n_max > 0x3fffffff)
         return ENL_E_LIMIT;
     const int row_tiles = ceil_div(a->n_max * c->rep, kTileRows);
-    const int64_t units = static_cast<int64_t>(B) * d.n_kv_heads * row_tiles;
-    if (units > 0x3fffffff || (B > 1 && (B > 0x7fff || d.n_kv_heads > 0xffff))) return ENL_E_LIMIT;
+    if (static_cast<int64_t>(B) * d.n_kv_heads * row_tiles * ENL_TREE_MAX_NODES > 0x3fffffff || (B > 1 && (B > 0x7fff || d.n_kv_heads > 0xffff))) return ENL_E_LIMIT;
 
     // ---- gather plan: the episodes' streams; reused when nothing it was built from has changed ----
     const size_t cu_bytes = sizeof(int32_t) * (B + 1);
@@ -72,70 +137,87 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
             for (int s = cu_sel[b]; s < cu_sel[b + 1]; ++s) e += std::max(1, ceil_div(c->sel_len[s], kPageTokens));
             n_entries += (e + kPagesPerTile - 1) / kPagesPerTile * kPagesPerTile;
         }
-        if (n_entries > c->cap_entries || (B > 1 && units > c->cap_items)) return ENL_E_NOMEM;
-        static_assert(sizeof(TreeItem) == sizeof(Item) && sizeof(int2) <= sizeof(EpInfo), "the plan buffers are made for these");
+        if (n_entries > c->cap_entries) return ENL_E_NOMEM;
 
-        // Splits.  The host does not know how long the tails are, so they count for what their tables hold: too many splits of a stream that
-        // turns out short cost little, since all CTAs run at once.  Two of them fit a multiprocessor; every request gets splits until they fill
-        // that many places (the longest streams first: ranges of as few pages as there are places for).
-        std::vector<int32_t> &ns = c->tree_splits;
-        ns.assign(B, 1);
-        auto pages_of = [&](int b) {
-            int64_t e = ceil_div(a->n_max, kPageTokens) + a->max_blocks;
-            for (int s = cu_sel[b]; s < cu_sel[b + 1]; ++s) e += std::max(1, ceil_div(c->sel_len[s], kPageTokens));
-            return e;
-        };
-        const int64_t per_request = static_cast<int64_t>(d.n_kv_heads) * row_tiles;
-        const int64_t slot_bytes = static_cast<int64_t>(kTileRows) * (d.head_dim + 1) * 4;
-        int64_t places = std::min<int64_t>(2 * c->n_sm, d.scratch_bytes / slot_bytes);
-        places = std::min<int64_t>(places, std::min(c->cap_items, 0xfff));      // (splits are twelve bits of an item)
-        if (units < places) {
-            int64_t lo = 1, hi = 1;                        // pages of a split: the fewest for which all CTAs have a place
-            for (int b = 0; b < B; ++b) hi = std::max(hi, pages_of(b));
+        // Shares of the CTAs.  The host does not know how long the tails are, so they count for what their tables hold: too many parts of a stream
+        // that turns out short cost little, since all CTAs run at once.  Two of them fit a multiprocessor.
+        const int64_t slot_bytes = static_cast<int64_t>(kTileRows) * (d.head_dim + 1) * 4 * row_tiles;
+        const int64_t places = std::max<int64_t>(1, 2 * c->n_sm / row_tiles), slots = d.scratch_bytes / slot_bytes;
+        std::vector<int64_t> pages(B), parts(B, 1);
+        for (int b = 0; b < B; ++b) {
+            pages[b] = ceil_div(a->n_max, kPageTokens) + static_cast<int64_t>(a->max_blocks);
+            for (int s = cu_sel[b]; s < cu_sel[b + 1]; ++s) pages[b] += std::max(1, ceil_div(c->sel_len[s], kPageTokens));
+        }
+        // equal parts: of as few pages as there are places for
+        const int64_t n_units = static_cast<int64_t>(B) * d.n_kv_heads, few = std::min(places, slots);
+        if (n_units < few) {
+            int64_t lo = 1, hi = *std::max_element(pages.begin(), pages.end());
             while (lo < hi) {
                 const int64_t mid = (lo + hi) / 2;
                 int64_t n = 0;
-                for (int b = 0; b < B; ++b) n += (pages_of(b) + mid - 1) / mid * per_request;
-                if (n <= places) hi = mid; else lo = mid + 1;
+                for (int b = 0; b < B; ++b) n += (pages[b] + mid - 1) / mid * d.n_kv_heads;
+                if (n <= few) hi = mid; else lo = mid + 1;
             }
-            for (int b = 0; b < B; ++b) ns[b] = splits_for(pages_of(b), (pages_of(b) + hi - 1) / hi);
+            for (int b = 0; b < B; ++b) parts[b] = parts_for(pages[b], (pages[b] + hi - 1) / hi);
         }
-        int64_t n_items = 0;
-        int most = 1;
-        for (int b = 0; b < B; ++b) {
-            n_items += ns[b] * per_request;
-            most = std::max(most, ns[b]);
+        Shares sh;
+        sh.heads = d.n_kv_heads;
+        int64_t n_groups = d.n_kv_heads * parts[0];
+        if (B > 1) {
+            // Equal parts leave places empty, or the longest streams with the longest parts (16 requests of 3200 cached keys and
+            // tails of 256 to 768, 8 kv heads: ... us); runs are as long for every CTA, but cost most CTAs a second segment.
+            int64_t total = 0, longest = 0, cut = 0;
+            std::vector<int64_t> steps(B);
+            for (int b = 0; b < B; ++b) {
+                steps[b] = steps_of(pages[b]);
+                total += steps[b] * d.n_kv_heads;
+                longest = std::max(longest, steps_of((pages[b] + parts[b] - 1) / parts[b]));
+                cut |= parts[b] > 1;
+            }
+            const int64_t waves = (n_units + places - 1) / places;
+            const int64_t by_parts = n_units > places ? std::max(longest, (total + places - 1) / places + (waves - 1) * kSegmentSteps + longest / 2)
+                                                      : longest + (cut ? kMergeSteps : 0);
+            const int64_t by_runs = (total + places - 1) / places + kSegmentSteps + kMergeSteps;
+            sh.units.assign(n_units, make_int2(0, 0));
+            if (by_runs < by_parts && 2 * places <= slots) sh.runs(steps, places);
+            else sh.equal(parts);
+            n_groups = static_cast<int64_t>(sh.off.size()) - 1;
         }
+        const size_t needed = B > 1 ? sizeof(TreeSegment) * sh.segments.size() + sizeof(int32_t) * (n_groups + 1) + sizeof(int2) * n_units + 64 : 0;
+        if (needed + 2 * (sizeof(int32_t) * n_entries + 16) > c->plan_bytes) return ENL_E_NOMEM;
 
         if (const int rc = open_plan(c)) return rc;
         size_t at = 0;
         auto section = [&](size_t bytes) { const size_t o = at; at += (bytes + 15) & ~static_cast<size_t>(15); return o; };
-        c->off_items = section(B > 1 ? sizeof(TreeItem) * n_items : 0);
-        c->off_eps = section(B > 1 ? sizeof(int2) * B : 0);
+        c->off_items = section(sizeof(TreeSegment) * sh.segments.size());
+        c->off_rowslots = section(B > 1 ? sizeof(int32_t) * (n_groups + 1) : 0);
+        c->off_eps = section(sizeof(int2) * sh.units.size());
         c->off_stream = section(sizeof(int32_t) * n_entries);
         c->off_meta = section(sizeof(int32_t) * n_entries);
         c->plan_used = at;
         int32_t ne = 0;
-        TreeItem *items = reinterpret_cast<TreeItem *>(c->plan_host + c->off_items);
-        int2 *heads = reinterpret_cast<int2 *>(c->plan_host + c->off_eps);
-        int32_t n_done = 0;
+        std::vector<EpInfo> eps(B);
         for (int b = 0; b < B; ++b) {
-            EpInfo e = {};
-            e.n_slots = cu_sel[b + 1] - cu_sel[b];
-            ne = write_stream(c, e, a->sel_ids + cu_sel[b], c->sel_len.data() + cu_sel[b], ne);
-            c->tree_entries = e.n_entries;
-            if (B == 1) break;
-            heads[b] = make_int2(n_done, ns[b]);
-            for (int h = 0; h < d.n_kv_heads; ++h)
-                for (int s = 0; s < ns[b]; ++s) {
-                    const int first = static_cast<int>(static_cast<int64_t>(e.n_entries) * s / ns[b]);
-                    const int last = static_cast<int>(static_cast<int64_t>(e.n_entries) * (s + 1) / ns[b]);
-                    for (int t = 0; t < row_tiles; ++t) items[n_done++] = TreeItem{b << 16 | h, t << 24 | s << 12 | ns[b], e.stream_off + first, last - first};
-                }
+            eps[b] = EpInfo{};
+            eps[b].n_slots = cu_sel[b + 1] - cu_sel[b];
+            ne = write_stream(c, eps[b], a->sel_ids + cu_sel[b], c->sel_len.data() + cu_sel[b], ne);
+        }
+        c->tree_entries = eps[0].n_entries;
+        if (B > 1) {
+            for (TreeSegment &g : sh.segments) {
+                const EpInfo &e = eps[g.head >> 16];
+                const int32_t first = static_cast<int32_t>(static_cast<int64_t>(e.n_entries) * g.from / g.whole);
+                g.first = e.stream_off + first;
+                g.count = static_cast<int32_t>(static_cast<int64_t>(e.n_entries) * g.to / g.whole) - first;
+            }
+            std::memcpy(c->plan_host + c->off_items, sh.segments.data(), sizeof(TreeSegment) * sh.segments.size());
+            std::memcpy(c->plan_host + c->off_rowslots, sh.off.data(), sizeof(int32_t) * sh.off.size());
+            std::memcpy(c->plan_host + c->off_eps, sh.units.data(), sizeof(int2) * sh.units.size());
         }
         c->plan_entries = ne;
-        c->plan_items = static_cast<int32_t>(n_items);
-        c->plan_splits = most;
+        c->plan_items = static_cast<int32_t>(n_groups * row_tiles);
+        c->plan_splits = B > 1 ? sh.most : static_cast<int32_t>(parts[0]);
+        c->tree_slots = B > 1 ? sh.slots : static_cast<int32_t>(n_groups);
         c->plan_batch = B;
         c->plan_epoch = c->epoch;
         c->plan_tree = true;
@@ -173,7 +255,8 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
     }
     p.tm_kpool = c->tm_k[a->layer];
     p.tm_vpool = c->tm_v[a->layer];
-    p.items = reinterpret_cast<const TreeItem *>(c->plan_dev + c->off_items);
+    p.segments = reinterpret_cast<const TreeSegment *>(c->plan_dev + c->off_items);
+    p.segment_off = reinterpret_cast<const int32_t *>(c->plan_dev + c->off_rowslots);
     p.stream_page = reinterpret_cast<const int32_t *>(c->plan_dev + c->off_stream);
     p.stream_meta = reinterpret_cast<const int32_t *>(c->plan_dev + c->off_meta);
     p.block_table = a->block_table;
@@ -195,7 +278,7 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(d.head_dim));
 
     p.part_o = c->scratch;
-    p.part_lse = c->scratch + static_cast<int64_t>(c->plan_items) * kTileRows * d.head_dim;
+    p.part_lse = c->scratch + static_cast<int64_t>(c->tree_slots) * row_tiles * kTileRows * d.head_dim;
     if (join_loads(c, st, a->layer) != ENL_OK) return ENL_E_CUDA;
     const unsigned long long graph = capture_of(st);
     if (send_plan(c, graph, st) != ENL_OK) return ENL_E_CUDA;
@@ -216,8 +299,7 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         mp.Hkv = d.n_kv_heads;
         mp.rep = c->rep;
         mp.row_tiles = row_tiles;
-        mp.row_groups = ceil_div(a->n_max * c->rep, 32);
-        if (launch_tree_merge(mp, d.head_dim, B, c->plan_splits > 4, st) != cudaSuccess) { cudaGetLastError(); return ENL_E_CUDA; }
+        if (launch_tree_merge(mp, d.head_dim, B, c->plan_splits, st) != cudaSuccess) { cudaGetLastError(); return ENL_E_CUDA; }
     }
     return ENL_OK;
 }

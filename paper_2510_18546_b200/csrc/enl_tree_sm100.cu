@@ -15,12 +15,12 @@
 // of its share of the memory; the tensor pipe needs 512 of them and the special-function units 512).  Hence two CTAs per
 // multiprocessor, whose chains scores -> softmax -> P V overlap, and splits that fill the device whatever the batch.
 //
-// Splits: the host knows the cached pages of a request, but not how long its tail is.  So it settles how many splits a request has, and split s of
-// ns takes pages [C s / ns, C (s + 1) / ns) of the C cached ones and the same part of the tail's and the nodes' pages, whose number the
-// device finds.  The cached pages of the first steps are fetched before the kernel waits for the one before it (plan and pool are written by the
-// library only); lengths are read while they are on their way.  (With shares that the device cut from the whole stream the first
-// scores were there 4.6 us after the wait for the previous kernel, for 16 requests 5.5, ...)  Splits leave outputs normalised by their own sums,
-// and log2-sum-exps, in the scratch buffer; tree_merge_kernel puts them together.
+// Shares: the host knows the cached pages of a request, but not how long its tail is.  So it cuts the stream of a request and kv head (a "unit")
+// by fractions: the part from a / E to b / E takes those pages of the C cached ones and the same part of the tail's and the nodes' pages, whose
+// number the device finds.  A CTA has one part, or, where the units do not divide into equal parts (see enl_tree.cu), a run of parts of
+// consecutive units that is as long as any other CTA's; the loads of a part run under the one before it.  The cached pages of the first steps are fetched before the
+// kernel waits for the one before it (plan and pool are written by the library only).
+// Parts of a unit leave outputs normalised by their own sums, and log2-sum-exps, in the scratch buffer; tree_merge_kernel puts them together.
 #include <cuda_bf16.h>
 
 #include "attn_ops.cuh"
@@ -53,7 +53,7 @@ struct Cfg {
     static constexpr int kKOff       = kTileBytes;
     static constexpr int kVOff       = kKOff + kRingK * kStepBytes;
     static constexpr int kBarOff     = kVOff + kRingV * kStepBytes;
-    static constexpr int kBars       = 7 + 2 * (kRingK + kRingV);
+    static constexpr int kBars       = 9 + 2 * (kRingK + kRingV);
     static constexpr int kSmemBytes  = kBarOff + 8 * kBars + 8;
     static_assert(kSmemBytes <= 115712, "two CTAs per multiprocessor");
 };
@@ -69,13 +69,16 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     const uint32_t bar0 = sbase + C::kBarOff;
-    const uint32_t bar_q_full = bar0, bar_pv_done = bar0 + 8u, bar_o_done = bar0 + 16u;      // P V of a step, of the last one
-    auto bar_s_full  = [&](int b) { return bar0 + 8u * (3 + b); };              // b: step & 1
-    auto bar_p_full  = [&](int b) { return bar0 + 8u * (5 + b); };
-    auto bar_k_full  = [&](int x) { return bar0 + 8u * (7 + x); };              // x: place in the ring
-    auto bar_k_empty = [&](int x) { return bar0 + 8u * (7 + C::kRingK + x); };
-    auto bar_v_full  = [&](int x) { return bar0 + 8u * (7 + 2 * C::kRingK + x); };
-    auto bar_v_empty = [&](int x) { return bar0 + 8u * (7 + 2 * C::kRingK + C::kRingV + x); };
+    const uint32_t bar_q_full = bar0, bar_q_empty = bar0 + 8u;                   // the Q tile of a segment is there / may be overwritten
+    const uint32_t bar_pv_done = bar0 + 16u, bar_o_done = bar0 + 24u;           // P V of a step / of a segment's last one
+    const uint32_t bar_o_free = bar0 + 32u;                                     // the accumulator has been read
+    auto bar_s_full  = [&](int b) { return bar0 + 8u * (5 + b); };              // b: step & 1
+    auto bar_p_full  = [&](int b) { return bar0 + 8u * (7 + b); };
+    auto bar_k_full  = [&](int x) { return bar0 + 8u * (9 + x); };              // x: place in the ring
+    auto bar_k_empty = [&](int x) { return bar0 + 8u * (9 + C::kRingK + x); };
+    auto bar_v_full  = [&](int x) { return bar0 + 8u * (9 + 2 * C::kRingK + x); };
+    auto bar_v_empty = [&](int x) { return bar0 + 8u * (9 + 2 * C::kRingK + C::kRingV + x); };
+    auto phase_of = [](int at, int places) { return static_cast<uint32_t>((at / places) & 1); };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kBarOff + 8 * C::kBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
 
@@ -84,23 +87,35 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
         return;
     }
     if (p.wait_first) pdl_wait();
-    // ---- what this CTA does: request, kv head, tile of rows, split; the cached pages of that split ----
-    struct { int b, kvh, rt, split, n_splits, first, count; } it;
-    if (p.batch == 1) {
-        const int idx = static_cast<int>(blockIdx.x), above = idx / p.row_tiles;
-        it.b = 0;
-        it.rt = idx - above * p.row_tiles;
-        it.kvh = above / p.n_splits;
-        it.split = above - it.kvh * p.n_splits;
-        it.n_splits = p.n_splits;
-        it.first = static_cast<int>(static_cast<long long>(p.n_entries) * it.split / p.n_splits);
-        it.count = static_cast<int>(static_cast<long long>(p.n_entries) * (it.split + 1) / p.n_splits) - it.first;
-    } else {
-        const int4 a = __ldcg(reinterpret_cast<const int4 *>(p.items) + blockIdx.x);
-        it.b = a.x >> 16; it.kvh = a.x & 0xffff;
-        it.rt = a.y >> 24; it.split = a.y >> 12 & 0xfff; it.n_splits = a.y & 0xfff;
-        it.first = a.z; it.count = a.w;
+    // ---- what this CTA does: a tile of rows of its segments (see TreeSegment) ----
+    const int group = p.row_tiles == 1 ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) / p.row_tiles;
+    const int rt = p.row_tiles == 1 ? 0 : static_cast<int>(blockIdx.x) - group * p.row_tiles;
+    struct Part { int b, kvh, slot, first, count, from, to, whole; };
+    auto segment = [&](int i) -> Part {
+        Part w;
+        if (p.batch == 1) {
+            w.b = 0;
+            w.kvh = group / p.n_splits;
+            w.from = group - w.kvh * p.n_splits;
+            w.to = w.from + 1;
+            w.whole = p.n_splits;
+            w.slot = p.n_splits > 1 ? group : -1;
+            w.first = static_cast<int>(static_cast<long long>(p.n_entries) * w.from / p.n_splits);
+            w.count = static_cast<int>(static_cast<long long>(p.n_entries) * w.to / p.n_splits) - w.first;
+        } else {
+            const int4 *src = reinterpret_cast<const int4 *>(p.segments + i);
+            const int4 x = __ldcg(src), y = __ldcg(src + 1);
+            w.b = x.x >> 16; w.kvh = x.x & 0xffff; w.slot = x.y; w.first = x.z; w.count = x.w;
+            w.from = y.x; w.to = y.y; w.whole = y.z;
+        }
+        return w;
+    };
+    int seg_beg = 0, seg_end = 1;
+    if (p.batch > 1) {
+        seg_beg = __ldcg(p.segment_off + group);
+        seg_end = __ldcg(p.segment_off + group + 1);
     }
+    Part it = segment(seg_beg);
 
     // ---- set-up ----
     if (warp == C::kMmaWarp) {
@@ -111,6 +126,8 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         mbar_init(bar_q_full, 1);
+        mbar_init(bar_q_empty, 1);
+        mbar_init(bar_o_free, C::kSoftmaxWarps);                  // (with rows or without)
         mbar_init(bar_pv_done, 1);
         mbar_init(bar_o_done, 1);
         for (int b = 0; b < 2; ++b) {
@@ -137,10 +154,15 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
         n = l0 < 0 ? 0 : max(0, min(n0, p.n_max));
         tail_pages = pages_of(len);
         const int t = tail_pages + pages_of(n);
-        t_first = static_cast<int>(static_cast<long long>(t) * it.split / it.n_splits);
-        t_count = static_cast<int>(static_cast<long long>(t) * (it.split + 1) / it.n_splits) - t_first;
-        n_steps = it.rt * kRows < n * p.rep ? (it.count + t_count + kStepPages - 1) / kStepPages : 0;
+        // (rising in `at`, 0 at 0 and t at the end: the parts of a unit meet)
+        auto cut = [&](int at) { return at >= it.whole ? t : min(t, static_cast<int>(static_cast<float>(t) * (static_cast<float>(at) / static_cast<float>(it.whole)))); };
+        t_first = cut(it.from);
+        t_count = cut(it.to) - t_first;
+        n_steps = rt * kRows < n * p.rep ? (it.count + t_count + kStepPages - 1) / kStepPages : 0;
     };
+    // The steps of cached pages alone that the ring has room for are fetched before the wait for the kernel before.  A first segment that turns
+    // out to have no rows leaves them, and its Q tile, to be passed over.
+    const int early_k = p.wait_first ? 0 : min(C::kRingK, it.count / kStepPages), early_v = p.wait_first ? 0 : min(C::kRingV, it.count / kStepPages);
 
     if (warp == C::kKWarp || warp == C::kVWarp) {
         // ================= TMA producers =================
@@ -149,7 +171,7 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                           *tm_new = is_k ? &p.tm_knew : &p.tm_vnew;
         const uint32_t ring = sbase + static_cast<uint32_t>(is_k ? C::kKOff : C::kVOff), full0 = is_k ? bar_k_full(0) : bar_v_full(0),
                        empty0 = is_k ? bar_k_empty(0) : bar_v_empty(0);
-        const int places = is_k ? C::kRingK : C::kRingV;
+        const int places = is_k ? C::kRingK : C::kRingV, early = is_k ? early_k : early_v;
         // Where pages lie, one per lane, fetched eight steps ahead: kind << 30 | page of the pool (0), of the tail (1), first row among the
         // request's nodes (2).  What fills the last step, and an entry of the block table that names no page, is the page of zeros.
         auto where = [&](int i) -> uint32_t {
@@ -178,55 +200,72 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                 }
             }
         };
-        // the steps of cached pages alone that the ring has room for, before the wait for the kernel before
-        const int early = p.wait_first ? 0 : min(places, it.count / kStepPages);
+        auto fetch_q = [&]() {
+            if (is_k && lane == 0) {
+                mbar_expect_tx(bar_q_full, static_cast<uint32_t>(C::kBlocks * p.box_tokens * p.rep * 128));
+                for (int b = 0; b < C::kBlocks; ++b)
+                    tma_load_3d(sbase + b * C::kBlockBytes, &p.tm_q, b * 64, it.kvh * p.rep, it.b * p.n_max + rt * (kRows / p.rep), bar_q_full);
+            }
+            __syncwarp();
+        };
+        static_assert(C::kRingK < kBatch && C::kRingV < kBatch, "the early steps' pages are of one batch");
         uint32_t cur = 0, next = where(lane);                        // (of the cached pages so far)
-        int jj = 0;
-        for (; jj < early; ++jj) fetch(__shfl_sync(kFull, next, jj * kStepPages + lane % kStepPages), jj);
+        int f = 0, qn = 1;                                           // steps fetched, Q tiles fetched
+        for (; f < early; ++f) fetch(__shfl_sync(kFull, next, f * kStepPages + lane % kStepPages), f);
+        pdl_wait();
+        fetch_q();
+        read_lengths();
+        for (int si = seg_beg; ok;) {
+            int jj = si == seg_beg && n_steps > 0 ? early : 0;
+            if (si > seg_beg) {
+                next = where(lane);
+                if (is_k && n_steps > 0) {
+                    ok = mbar_wait(bar_q_empty, static_cast<uint32_t>((qn - 1) & 1), abort_flag, p.status);
+                    if (!ok) break;
+                    fetch_q();
+                    ++qn;
+                }
+            } else if (lane >= it.count) {
+                next = where(lane);
+            }
+            cur = next;
+            if (jj > 0) next = where(kBatch * kStepPages + lane);
+            for (; jj < n_steps; ++jj) {
+                const int x = f % places;
+                if (jj % kBatch == 0) {
+                    cur = next;
+                    next = where((jj + kBatch) * kStepPages + lane);
+                }
+                const uint32_t at = __shfl_sync(kFull, cur, jj % kBatch * kStepPages + lane % kStepPages);
+                if (f >= places) ok = mbar_wait(empty0 + 8u * x, phase_of(f, places) ^ 1u, abort_flag, p.status);
+                if (!ok) break;
+                fetch(at, x);
+                ++f;
+            }
+            if (++si >= seg_end) break;
+            it = segment(si);
+            read_lengths();
+        }
+        // error path only: copies in flight land before the CTA retires
+        if (!ok) {
+            for (int e = max(0, f - places); e < f; ++e) {
+                const unsigned long long t0 = global_ns();
+                while (!mbar_try_wait(full0 + 8u * (e % places), phase_of(e, places)) && global_ns() - t0 < 2000000ull) { }
+            }
+        }
+    } else if (warp == C::kMmaWarp) {
+        // ================= MMA issuer =================
         pdl_wait();
         read_lengths();
-        if (n_steps > 0 && is_k && lane == 0) {
-            mbar_expect_tx(bar_q_full, static_cast<uint32_t>(C::kBlocks * p.box_tokens * p.rep * 128));
-            for (int b = 0; b < C::kBlocks; ++b)
-                tma_load_3d(sbase + b * C::kBlockBytes, &p.tm_q, b * 64, it.kvh * p.rep, it.b * p.n_max + it.rt * (kRows / p.rep), bar_q_full);
-        }
-        __syncwarp();
-        if (lane >= it.count) next = where(lane);
-        static_assert(C::kRingK < kBatch && C::kRingV < kBatch, "the early steps' pages are of one batch");
-        cur = next;
-        if (jj > 0) next = where(kBatch * kStepPages + lane);
-        for (; jj < n_steps; ++jj) {
-            const int x = jj % places;
-            if (jj % kBatch == 0) {
-                cur = next;
-                next = where((jj + kBatch) * kStepPages + lane);
-            }
-            const uint32_t at = __shfl_sync(kFull, cur, jj % kBatch * kStepPages + lane % kStepPages);
-            if (jj >= places) ok = mbar_wait(empty0 + 8u * x, static_cast<uint32_t>((jj / places - 1) & 1), abort_flag, p.status);
-            if (!ok) break;
-            fetch(at, x);
-        }
-        // Copies in flight land before the CTA retires: on the error path, and where there turned out to be nothing to do.
-        if (!ok || n_steps == 0) {
-            for (int f = max(0, jj - places); f < jj; ++f) {
-                const unsigned long long t0 = global_ns();
-                while (!mbar_try_wait(full0 + 8u * (f % places), static_cast<uint32_t>((f / places) & 1)) && global_ns() - t0 < 2000000ull) { }
-            }
-        }
-    } else {
-      pdl_wait();
-      read_lengths();
-      if (n_steps > 0 && warp == C::kMmaWarp) {
-        // ================= MMA issuer =================
         constexpr uint32_t idesc_qk = make_idesc(kStepKeys, false), idesc_pv = make_idesc(D, true);
         constexpr uint32_t kStepUnits = C::kStepBytes >> 4, kGroupUnits = C::kGroupBytes >> 4;
         const uint64_t dq0 = smem_desc(sbase, 16), dk0 = smem_desc(sbase + C::kKOff, 16, C::kGroupBytes), dv0 = smem_desc(sbase + C::kVOff, 1024, C::kGroupBytes);
         const uint32_t dq_lo = static_cast<uint32_t>(dq0), dq_hi = static_cast<uint32_t>(dq0 >> 32);
         const uint32_t dk_lo = static_cast<uint32_t>(dk0), dk_hi = static_cast<uint32_t>(dk0 >> 32);
         const uint32_t dv_lo = static_cast<uint32_t>(dv0), dv_hi = static_cast<uint32_t>(dv0 >> 32);
-        // A commit that frees a place of the ring is made only where a later fetch waits for it: nothing may arrive after the CTA has retired.
-        auto issue_qk = [&](int jj) {
-            const int x = jj % C::kRingK, b = jj & 1;
+        int fk = 0, fv = 0, g = 0, qn = 0, on = 0;                  // steps whose K, whose V has been used, steps, Q tiles and accumulators so far
+        auto issue_qk = [&](int at, bool last) {                     // step `at` of all
+            const int x = fk % C::kRingK, b = at & 1;
             const uint32_t ka = dk_lo + static_cast<uint32_t>(x) * kStepUnits, d = tmem_base + static_cast<uint32_t>(b * kStepKeys);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
@@ -235,219 +274,271 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                         ka + static_cast<uint32_t>((kk >> 2) * (1024 >> 4)) + in_row, dk_hi, idesc_qk, kk > 0 ? 1u : 0u);
             }
             tc_commit(bar_s_full(b));
-            if (jj + C::kRingK < n_steps) tc_commit(bar_k_empty(x));
+            tc_commit(bar_k_empty(x));
+            if (last) tc_commit(bar_q_empty);
+            ++fk;
         };
         // O (+)= P V; P of keys 2c, 2c + 1 sits in column c of the buffer that held their scores
-        auto issue_pv = [&](int jj) {
-            const int x = jj % C::kRingV, b = jj & 1;
+        auto issue_pv = [&](bool first, bool last) {
+            const int x = fv % C::kRingV, b = g & 1;
             const uint32_t va = dv_lo + static_cast<uint32_t>(x) * kStepUnits, a = tmem_base + static_cast<uint32_t>(b * kStepKeys);
 #pragma unroll
             for (int k4 = 0; k4 < kStepPages; ++k4)                  // 16 keys = two groups of 8 rows, 8 columns of P
                 mma_ts2(tmem_base + kOCol, a + static_cast<uint32_t>(k4 * 8), va + static_cast<uint32_t>(k4 * 2) * kGroupUnits, dv_hi, idesc_pv,
-                        (jj == 0 && k4 == 0) ? 0u : 1u);
-            if (jj + C::kRingV < n_steps) tc_commit(bar_v_empty(x));
-            tc_commit(jj + 1 < n_steps ? bar_pv_done : bar_o_done);
+                        (first && k4 == 0) ? 0u : 1u);
+            tc_commit(bar_v_empty(x));
+            tc_commit(last ? bar_o_done : bar_pv_done);
+            ++fv;
         };
-        auto wait_k = [&](int jj) { return mbar_wait(bar_k_full(jj % C::kRingK), static_cast<uint32_t>((jj / C::kRingK) & 1), abort_flag, p.status); };
-        ok = mbar_wait(bar_q_full, 0, abort_flag, p.status);
-        for (int jj = 0; jj < min(2, n_steps) && ok; ++jj) {
-            ok = wait_k(jj);
-            if (!ok) break;
-            tc_fence_after();
-            issue_qk(jj);
+        auto wait_k = [&]() { return mbar_wait(bar_k_full(fk % C::kRingK), phase_of(fk, C::kRingK), abort_flag, p.status); };
+        auto wait_v = [&]() { return mbar_wait(bar_v_full(fv % C::kRingV), phase_of(fv, C::kRingV), abort_flag, p.status); };
+        for (int si = seg_beg; ok;) {
+            if (si == seg_beg || n_steps > 0) {
+                ok = mbar_wait(bar_q_full, static_cast<uint32_t>(qn & 1), abort_flag, p.status);
+                ++qn;
+            }
+            if (n_steps == 0 && si == seg_beg) {                     // what was fetched for nothing
+                for (int e = 0; e < early_k && ok; ++e, ++fk) {
+                    ok = wait_k();
+                    if (lane == 0) mbar_arrive(bar_k_empty(fk % C::kRingK));
+                }
+                for (int e = 0; e < early_v && ok; ++e, ++fv) {
+                    ok = wait_v();
+                    if (lane == 0) mbar_arrive(bar_v_empty(fv % C::kRingV));
+                }
+                if (lane == 0) mbar_arrive(bar_q_empty);
+            }
+            for (int jj = 0; jj < min(2, n_steps) && ok; ++jj) {
+                ok = wait_k();
+                if (!ok) break;
+                tc_fence_after();
+                issue_qk(g + jj, jj + 1 == n_steps);
+            }
+            for (int jj = 0; jj < n_steps && ok; ++jj, ++g) {
+                const bool more = jj + 2 < n_steps;
+                ok = wait_v();
+                if (ok && more) ok = wait_k();
+                if (ok && jj == 0 && on > 0) ok = mbar_wait(bar_o_free, static_cast<uint32_t>((on - 1) & 1), abort_flag, p.status);
+                if (ok) ok = mbar_wait(bar_p_full(g & 1), static_cast<uint32_t>((g >> 1) & 1), abort_flag, p.status);
+                if (!ok) break;
+                tc_fence_after();
+                issue_pv(jj == 0, jj + 1 == n_steps);
+                if (more) issue_qk(g + 2, jj + 3 == n_steps);
+            }
+            if (n_steps > 0) ++on;
+            if (++si >= seg_end) break;
+            it = segment(si);
+            read_lengths();
         }
-        for (int jj = 0; jj < n_steps && ok; ++jj) {
-            const bool more = jj + 2 < n_steps;
-            ok = mbar_wait(bar_v_full(jj % C::kRingV), static_cast<uint32_t>((jj / C::kRingV) & 1), abort_flag, p.status);
-            if (ok && more) ok = wait_k(jj + 2);
-            if (ok) ok = mbar_wait(bar_p_full(jj & 1), static_cast<uint32_t>((jj >> 1) & 1), abort_flag, p.status);
-            if (!ok) break;
-            tc_fence_after();
-            issue_pv(jj);
-            if (more) issue_qk(jj + 2);
-        }
-        if (ok) ok = mbar_wait(bar_o_done, 0, abort_flag, p.status);
-      } else if (warp < C::kSoftmaxWarps && it.rt * kRows + warp * 32 < n * p.rep) {
+        // nothing may arrive after the CTA has retired
+        for (int e = max(0, fk - C::kRingK); e < fk && ok; ++e) ok = mbar_wait(bar_k_empty(e % C::kRingK), phase_of(e, C::kRingK), abort_flag, p.status);
+        for (int e = max(0, fv - C::kRingV); e < fv && ok; ++e) ok = mbar_wait(bar_v_empty(e % C::kRingV), phase_of(e, C::kRingV), abort_flag, p.status);
+        if (ok) ok = mbar_wait(bar_q_empty, static_cast<uint32_t>((qn - 1) & 1), abort_flag, p.status);
+        if (ok && on > 0) ok = mbar_wait(bar_o_done, static_cast<uint32_t>((on - 1) & 1), abort_flag, p.status);
+    } else {
         // ================= softmax: one thread per query row =================
         const int rep = p.rep, lr = 31 - __clz(rep);
-        const int r = warp * 32 + lane, n_act = (min(kRows, n * rep - it.rt * kRows) + 31) >> 5;      // softmax warps with rows
-        const int t = it.rt * (kRows >> lr) + (r >> lr);              // node
-        const bool row_valid = t < n;
+        const int r = warp * 32 + lane;
+        const int t = rt * (kRows >> lr) + (r >> lr);                 // node
         const uint32_t lane_sel = static_cast<uint32_t>(warp * 32) << 16;
         const uint32_t t_s = tmem_base + lane_sel, t_o = tmem_base + lane_sel + kOCol;
         const float scale = p.scale_log2;
-        // nodes that this one sees; without masks the nodes are a chain
-        unsigned long long tree = 0;
-        if (row_valid) {
-            tree = p.mask ? __ldcg(p.mask + static_cast<long long>(it.b) * p.n_max + t) : (2ull << t) - 1ull;
-            if (n < 64) tree &= (1ull << n) - 1ull;
-        }
-        // Keys of 32 pages, one page per lane, fetched eight steps ahead: how many of the page's rows count, or 256 | first node of a page of nodes.
-        auto load_meta = [&](int i) -> int {
-            if (i < it.count) return __ldcg(p.stream_meta + it.first + i) & 0xff;
-            const int g = i - it.count + t_first;
-            if (i >= it.count + t_count) return 0;
-            return g < tail_pages ? min(kPageTokens, len - g * kPageTokens) : 256 | (g - tail_pages) * kPageTokens;
-        };
-        int meta = 0, meta_next = n_steps > 0 ? load_meta(lane) : 0;
-        float m = kNegInf, l = 0.f;                                   // reference (log2 units), row sum
-        for (int jj = 0; jj < n_steps; ++jj) {
-            const int b = jj & 1;
-            if (jj % kBatch == 0) {
-                meta = meta_next;
-                meta_next = load_meta((jj + kBatch) * kStepPages + lane);
-            }
-            int pg[kStepPages];
-            bool whole = true;
-#pragma unroll
-            for (int e = 0; e < kStepPages; ++e) {
-                pg[e] = __shfl_sync(kFull, meta, jj % kBatch * kStepPages + e);
-                whole = whole && pg[e] == kPageTokens;
-            }
-            const uint32_t t_sb = t_s + static_cast<uint32_t>(b * kStepKeys);
-            ok = mbar_wait(bar_s_full(b), static_cast<uint32_t>((jj >> 1) & 1), abort_flag, p.status);
-            if (!ok) break;
-            tc_fence_after();
-
-            // the row's 64 scores
-            uint32_t su[kStepKeys];
-#pragma unroll
-            for (int k = 0; k < kStepKeys / 32; ++k)
-                tmem_ld32_issue(t_sb + static_cast<uint32_t>(k * 32), reinterpret_cast<uint32_t(&)[32]>(su[k * 32]));
-            tmem_ld_wait();
-#pragma unroll
-            for (int k = 0; k < kStepKeys / 32; ++k) tmem_ld32_arrived(reinterpret_cast<uint32_t(&)[32]>(su[k * 32]));
-            float s[kStepKeys];
-#pragma unroll
-            for (int x = 0; x < kStepKeys; ++x) s[x] = __uint_as_float(su[x]);
-
-            // Hide what does not count: rows behind the end of a page's, and nodes that are no ancestors.  By a select, not by adding -inf: keys
-            // that nobody sees may hold anything.
-            if (!whole) {
-#pragma unroll
-                for (int e = 0; e < kStepPages; ++e) {
-                    const uint32_t see = pg[e] & 256 ? static_cast<uint32_t>(tree >> (pg[e] & 63)) : (1u << pg[e]) - 1u;
-#pragma unroll
-                    for (int x = 0; x < kPageTokens; ++x)
-                        if (!((see >> x) & 1u)) s[e * kPageTokens + x] = kNegInf;
+        int g0 = 0, fv0 = 0, on = 0;                                  // steps, steps whose V was fetched, accumulators of the segments before
+        pdl_wait();
+        read_lengths();
+        for (int si = seg_beg; ok;) {
+            if (n_steps == 0 && si == seg_beg) fv0 = early_v;
+            if (rt * kRows + warp * 32 < n * rep) {
+                const int n_act = (min(kRows, n * rep - rt * kRows) + 31) >> 5;      // softmax warps with rows
+                const uint32_t arrivals = warp == 0 ? static_cast<uint32_t>(C::kSoftmaxWarps + 1 - n_act) : 1u;
+                const bool row_valid = t < n;
+                // nodes that this one sees; without masks the nodes are a chain
+                unsigned long long tree = 0;
+                if (row_valid) {
+                    tree = p.mask ? __ldcg(p.mask + static_cast<long long>(it.b) * p.n_max + t) : (2ull << t) - 1ull;
+                    if (n < 64) tree &= (1ull << n) - 1ull;
                 }
-            }
-
-            // row maximum: four independent chains
-            float mx4[kStepPages];
+                // Keys of 32 pages, one page per lane, fetched eight steps ahead: how many of the page's rows count, or 256 | first node of a page of nodes.
+                auto load_meta = [&](int i) -> int {
+                    if (i < it.count) return __ldcg(p.stream_meta + it.first + i) & 0xff;
+                    const int g = i - it.count + t_first;
+                    if (i >= it.count + t_count) return 0;
+                    return g < tail_pages ? min(kPageTokens, len - g * kPageTokens) : 256 | (g - tail_pages) * kPageTokens;
+                };
+                int meta = 0, meta_next = load_meta(lane);
+                float m = kNegInf, l = 0.f;                                   // reference (log2 units), row sum
+                for (int jj = 0; jj < n_steps; ++jj) {
+                    const int g = g0 + jj, b = g & 1;
+                    if (jj % kBatch == 0) {
+                        meta = meta_next;
+                        meta_next = load_meta((jj + kBatch) * kStepPages + lane);
+                    }
+                    int pg[kStepPages];
+                    bool whole = true;
 #pragma unroll
-            for (int k = 0; k < kStepPages; ++k) {
-                float a = fmax3(s[k * 16], s[k * 16 + 1], s[k * 16 + 2]);
-#pragma unroll
-                for (int x = 3; x < 15; x += 2) a = fmax3(a, s[k * 16 + x], s[k * 16 + x + 1]);
-                mx4[k] = fmaxf(a, s[k * 16 + 15]);
-            }
-            const float m_cand = fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
-
-            // The reference moves only when the row maximum has grown by more than the threshold; then sum and accumulator are
-            // rescaled, behind P V of the step before (the one before that was done when these scores were).
-            // (Rows of the tile that are no nodes hold whatever lay in shared memory: they must not move the others' references, or results
-            // would differ in their last bits from run to run.)
-            const bool need = row_valid && m_cand > m + kRescaleThreshold;       // also true when m == -inf < m_cand
-            if (__any_sync(kFull, need)) {
-                const float m_new = fmaxf(m, m_cand);
-                const float alpha = (m_new == kNegInf) ? 1.f : ex2(m - m_new);
-                l *= alpha;
-                m = m_new;
-                if (jj > 0) {
-                    ok = mbar_wait(bar_pv_done, static_cast<uint32_t>((jj - 1) & 1), abort_flag, p.status);
+                    for (int e = 0; e < kStepPages; ++e) {
+                        pg[e] = __shfl_sync(kFull, meta, jj % kBatch * kStepPages + e);
+                        whole = whole && pg[e] == kPageTokens;
+                    }
+                    const uint32_t t_sb = t_s + static_cast<uint32_t>(b * kStepKeys);
+                    ok = mbar_wait(bar_s_full(b), static_cast<uint32_t>((g >> 1) & 1), abort_flag, p.status);
                     if (!ok) break;
                     tc_fence_after();
+
+                    // the row's 64 scores
+                    uint32_t su[kStepKeys];
+#pragma unroll
+                    for (int k = 0; k < kStepKeys / 32; ++k)
+                        tmem_ld32_issue(t_sb + static_cast<uint32_t>(k * 32), reinterpret_cast<uint32_t(&)[32]>(su[k * 32]));
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int k = 0; k < kStepKeys / 32; ++k) tmem_ld32_arrived(reinterpret_cast<uint32_t(&)[32]>(su[k * 32]));
+                    float s[kStepKeys];
+#pragma unroll
+                    for (int x = 0; x < kStepKeys; ++x) s[x] = __uint_as_float(su[x]);
+
+                    // Hide what does not count: rows behind the end of a page's, and nodes that are no ancestors.  By a select, not by adding -inf: keys
+                    // that nobody sees may hold anything.
+                    if (!whole) {
+#pragma unroll
+                        for (int e = 0; e < kStepPages; ++e) {
+                            const uint32_t see = pg[e] & 256 ? static_cast<uint32_t>(tree >> (pg[e] & 63)) : (1u << pg[e]) - 1u;
+#pragma unroll
+                            for (int x = 0; x < kPageTokens; ++x)
+                                if (!((see >> x) & 1u)) s[e * kPageTokens + x] = kNegInf;
+                        }
+                    }
+
+                    // row maximum: four independent chains
+                    float mx4[kStepPages];
+#pragma unroll
+                    for (int k = 0; k < kStepPages; ++k) {
+                        float a = fmax3(s[k * 16], s[k * 16 + 1], s[k * 16 + 2]);
+#pragma unroll
+                        for (int x = 3; x < 15; x += 2) a = fmax3(a, s[k * 16 + x], s[k * 16 + x + 1]);
+                        mx4[k] = fmaxf(a, s[k * 16 + 15]);
+                    }
+                    const float m_cand = fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
+
+                    // The reference moves only when the row maximum has grown by more than the threshold; then sum and accumulator are
+                    // rescaled, behind P V of the step before (the one before that was done when these scores were; the last of a segment counts elsewhere).
+                    // (Rows of the tile that are no nodes hold whatever lay in shared memory: they must not move the others' references, or results
+                    // would differ in their last bits from run to run.)
+                    const bool need = row_valid && m_cand > m + kRescaleThreshold;       // also true when m == -inf < m_cand
+                    if (__any_sync(kFull, need)) {
+                        const float m_new = fmaxf(m, m_cand);
+                        const float alpha = (m_new == kNegInf) ? 1.f : ex2(m - m_new);
+                        l *= alpha;
+                        m = m_new;
+                        if (jj > 0) {
+                            ok = mbar_wait(bar_pv_done, static_cast<uint32_t>((g - on - 1) & 1), abort_flag, p.status);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll 1
+                            for (int k = 0; k < D / 32; ++k) {
+                                uint32_t o[32];
+                                tmem_ld32_wait(t_o + static_cast<uint32_t>(k * 32), o);
+#pragma unroll
+                                for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
+                                tmem_st32(t_o + static_cast<uint32_t>(k * 32), o);
+                            }
+                        }
+                    }
+                    const float m_use = (m == kNegInf) ? 0.f : m;
+
+                    // p = exp2(s * scale - m), summed in fp32 and rounded to bf16 for the tensor cores (as every kernel of the library does)
+                    const uint64_t sc2 = pack2(scale, scale), nm2 = pack2(-m_use, -m_use);
+                    uint64_t ps2[2];
+#pragma unroll
+                    for (int ch = 0; ch < kStepKeys / 32; ++ch) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) {
+                            float a0, a1;
+                            unpack2(fma2(pack2(s[ch * 32 + 2 * x], s[ch * 32 + 2 * x + 1]), sc2, nm2), a0, a1);
+                            a0 = ex2(a0);
+                            a1 = ex2(a1);
+                            const uint64_t p2 = pack2(a0, a1);
+                            pk[x] = pack_bf16(a0, a1);
+                            ps2[ch] = x ? add2(ps2[ch], p2) : p2;
+                        }
+                        tmem_st16(t_sb + static_cast<uint32_t>(ch * 16), pk);
+                    }
+                    // V rows that no row of the tile sees are cleared: 0 times whatever lies there must stay 0.  Those of the tail's last page and
+                    // behind the last node (pool pages are zero behind a group's end).
+                    if (!whole && warp == 0) {
+                        const int fv = fv0 + g, x = fv % C::kRingV;
+                        bool waited = false;
+#pragma unroll
+                        for (int e = 0; e < kStepPages; ++e) {
+                            const int rows = pg[e] & 256 ? min(kPageTokens, n - (pg[e] & 63)) : pg[e];
+                            if (jj * kStepPages + e < it.count || rows == 0 || rows == kPageTokens) continue;
+                            if (!waited) ok = mbar_wait(bar_v_full(x), phase_of(fv, C::kRingV), abort_flag, p.status);
+                            waited = true;
+                            if (!ok) break;
+                            uint8_t *page = smem + C::kVOff + x * C::kStepBytes + e * 2 * C::kGroupBytes;
+                            for (int i = lane; i < (kPageTokens - rows) * C::kBlocks * 8; i += 32) {    // 16-byte pieces
+                                const int row = rows + i / (C::kBlocks * 8), blk = i / 8 % C::kBlocks;
+                                *reinterpret_cast<uint4 *>(page + (row >> 3) * C::kGroupBytes + blk * 1024 + (row & 7) * 128 + i % 8 * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            }
+                        }
+                        if (!ok) break;
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_n(bar_p_full(b), arrivals);
+                    float lo0, hi0, lo1, hi1;
+                    unpack2(ps2[0], lo0, hi0);
+                    unpack2(ps2[1], lo1, hi1);
+                    l += (lo0 + hi0) + (lo1 + hi1);
+                }
+                if (n_steps == 0) {                                           // a part without a step: the rows have seen nothing of it
+                    if (it.slot >= 0) p.part_lse[(static_cast<long long>(it.slot) * p.row_tiles + rt) * kTileRows + r] = kNegInf;
+                } else if (ok && (ok = mbar_wait(bar_o_done, static_cast<uint32_t>(on & 1), abort_flag, p.status))) {
+                    tc_fence_after();
+                    const float inv = l > 0.f ? 1.f / l : 0.f;
+                    const bool split = it.slot >= 0;
+                    const long long slot = static_cast<long long>(it.slot) * p.row_tiles + rt;
+                    if (split) p.part_lse[slot * kTileRows + r] = l > 0.f ? m + lg2(l) : kNegInf;
+                    // partial outputs [slot][D / 4][row][4]: a warp's store is one contiguous piece
+                    float4 *part = reinterpret_cast<float4 *>(p.part_o) + slot * (D / 4) * kTileRows + r;
+                    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
+                                 ((static_cast<long long>(it.b) * p.n_max + t) * p.Hq + it.kvh * rep + (r & (rep - 1))) * D);
 #pragma unroll 1
                     for (int k = 0; k < D / 32; ++k) {
                         uint32_t o[32];
                         tmem_ld32_wait(t_o + static_cast<uint32_t>(k * 32), o);
+                        float f[32];
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
-                        tmem_st32(t_o + static_cast<uint32_t>(k * 32), o);
+                        for (int x = 0; x < 32; ++x) f[x] = l > 0.f ? __uint_as_float(o[x]) * inv : 0.f;      // a row that sees nothing: 0
+                        if (split) {
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) part[(k * 8 + x) * kTileRows] = make_float4(f[4 * x], f[4 * x + 1], f[4 * x + 2], f[4 * x + 3]);
+                        } else if (row_valid) {
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                dst[k * 4 + x] = make_uint4(pack_bf16(f[8 * x], f[8 * x + 1]), pack_bf16(f[8 * x + 2], f[8 * x + 3]),
+                                                            pack_bf16(f[8 * x + 4], f[8 * x + 5]), pack_bf16(f[8 * x + 6], f[8 * x + 7]));
+                        }
                     }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_o_free);
                 }
+            } else if (n_steps > 0) {
+                // A warp without rows in this segment may have some in the next.  It keeps step with the others: ahead of them it would take phases
+                // before for those that it waits for, and arrive where the first warp has arrived for it; two segments behind it would wait for good.
+                ok = mbar_wait(bar_o_done, static_cast<uint32_t>(on & 1), abort_flag, p.status);
+                if (ok && lane == 0) mbar_arrive(bar_o_free);
             }
-            const float m_use = (m == kNegInf) ? 0.f : m;
-
-            // p = exp2(s * scale - m), summed in fp32 and rounded to bf16 for the tensor cores (as every kernel of the library does)
-            const uint64_t sc2 = pack2(scale, scale), nm2 = pack2(-m_use, -m_use);
-            uint64_t ps2[2];
-#pragma unroll
-            for (int ch = 0; ch < kStepKeys / 32; ++ch) {
-                uint32_t pk[16];
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    float a0, a1;
-                    unpack2(fma2(pack2(s[ch * 32 + 2 * x], s[ch * 32 + 2 * x + 1]), sc2, nm2), a0, a1);
-                    a0 = ex2(a0);
-                    a1 = ex2(a1);
-                    const uint64_t p2 = pack2(a0, a1);
-                    pk[x] = pack_bf16(a0, a1);
-                    ps2[ch] = x ? add2(ps2[ch], p2) : p2;
-                }
-                tmem_st16(t_sb + static_cast<uint32_t>(ch * 16), pk);
-            }
-            // V rows that no row of the tile sees are cleared: 0 times whatever lies there must stay 0.  Those of the tail's last page and
-            // behind the last node (pool pages are zero behind a group's end).
-            if (!whole && warp == 0) {
-                const int x = jj % C::kRingV;
-                bool waited = false;
-#pragma unroll
-                for (int e = 0; e < kStepPages; ++e) {
-                    const int rows = pg[e] & 256 ? min(kPageTokens, n - (pg[e] & 63)) : pg[e];
-                    if (jj * kStepPages + e < it.count || rows == 0 || rows == kPageTokens) continue;
-                    if (!waited) ok = mbar_wait(bar_v_full(x), static_cast<uint32_t>((jj / C::kRingV) & 1), abort_flag, p.status);
-                    waited = true;
-                    if (!ok) break;
-                    uint8_t *page = smem + C::kVOff + x * C::kStepBytes + e * 2 * C::kGroupBytes;
-                    for (int i = lane; i < (kPageTokens - rows) * C::kBlocks * 8; i += 32) {    // 16-byte pieces
-                        const int row = rows + i / (C::kBlocks * 8), blk = i / 8 % C::kBlocks;
-                        *reinterpret_cast<uint4 *>(page + (row >> 3) * C::kGroupBytes + blk * 1024 + (row & 7) * 128 + i % 8 * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                }
-                if (!ok) break;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_n(bar_p_full(b), warp == 0 ? static_cast<uint32_t>(C::kSoftmaxWarps + 1 - n_act) : 1u);
-            float lo0, hi0, lo1, hi1;
-            unpack2(ps2[0], lo0, hi0);
-            unpack2(ps2[1], lo1, hi1);
-            l += (lo0 + hi0) + (lo1 + hi1);
+            if (n_steps > 0) ++on;
+            g0 += n_steps;
+            if (++si >= seg_end) break;
+            it = segment(si);
+            read_lengths();
         }
-        if (ok && n_steps > 0) ok = mbar_wait(bar_o_done, 0, abort_flag, p.status);
-        if (ok) {
-            tc_fence_after();
-            // (A split without a step has seen nothing, and O holds nothing: 0, as for a row that sees no key.)
-            const float inv = l > 0.f ? 1.f / l : 0.f;
-            const bool split = it.n_splits > 1;
-            if (split) p.part_lse[static_cast<long long>(blockIdx.x) * kTileRows + r] = l > 0.f ? m + lg2(l) : kNegInf;
-            // partial outputs [CTA][D / 4][row][4]: a warp's store is one contiguous piece
-            float4 *part = reinterpret_cast<float4 *>(p.part_o) + static_cast<long long>(blockIdx.x) * (D / 4) * kTileRows + r;
-            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
-                         ((static_cast<long long>(it.b) * p.n_max + t) * p.Hq + it.kvh * rep + (r & (rep - 1))) * D);
-#pragma unroll 1
-            for (int k = 0; k < D / 32; ++k) {
-                uint32_t o[32];
-                tmem_ld32_wait(t_o + static_cast<uint32_t>(k * 32), o);
-                float f[32];
-#pragma unroll
-                for (int x = 0; x < 32; ++x) f[x] = l > 0.f ? __uint_as_float(o[x]) * inv : 0.f;
-                if (split) {
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) part[(k * 8 + x) * kTileRows] = make_float4(f[4 * x], f[4 * x + 1], f[4 * x + 2], f[4 * x + 3]);
-                } else if (row_valid) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        dst[k * 4 + x] = make_uint4(pack_bf16(f[8 * x], f[8 * x + 1]), pack_bf16(f[8 * x + 2], f[8 * x + 3]),
-                                                    pack_bf16(f[8 * x + 4], f[8 * x + 5]), pack_bf16(f[8 * x + 6], f[8 * x + 7]));
-                }
-            }
-        }
-      }
     }
 
     // ---- teardown ----
@@ -459,52 +550,46 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
     }
 }
 
-// Puts the splits of a row together: out = sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M), in the order of the splits.  A CTA takes 32 rows of a
-// unit, a lane each; grid.x runs over units and groups of 32 rows, grid.y over channels.  Few registers and little shared memory: its
-// CTAs find a place beside those of the attention kernel and wait there for its end (with 512 threads of 64 registers they started
-// after it: 4.7 us behind it for one token of 8 kv heads, ...).
-//   kDeep: four channels a CTA; its warps take every fourth split, six of them at a time, and are added up in shared memory
-//   else (calls with many units, whose streams have few splits): sixteen channels a CTA, four a warp, which takes all splits
+// Puts the parts of a unit together: out = sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  A warp takes four channels of 32 / kLanes rows; kLanes
+// lanes share a row and take every kLanes-th part, up to kAhead at a time, all of whose loads are on their way at once.  No shared memory and few
+// registers, so that its CTAs find a place beside those of the attention kernel and wait there for its end; nor does a load wait for
+// another (a row that turns out to be none has read what lay in the scratch buffer).  grid.x: units and groups of rows, grid.y: channels.
 constexpr int kMergeWarps = 4;
-template <int D, bool kDeep>
+template <int D, int kLanes, int kAhead>
 __global__ void __launch_bounds__(kMergeWarps * 32, 8) tree_merge_kernel(const __grid_constant__ TreeMergeParams p)
 {
-    __shared__ float4 sums[kMergeWarps][32];
-    __shared__ float2 refs[kMergeWarps][32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kWarpRows = 32 / kLanes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, of = lane / kWarpRows;
     const int lr = 31 - __clz(p.rep);
-    const int row_groups = p.row_groups, b = static_cast<int>(blockIdx.x) / (p.Hkv * row_groups), at = static_cast<int>(blockIdx.x) - b * (p.Hkv * row_groups);
-    const int kvh = at / row_groups, rows0 = (at - kvh * row_groups) * 32, tile = rows0 / kTileRows;      // (calls of fewer rows have one tile)
-    const int quad = kDeep ? static_cast<int>(blockIdx.y) : static_cast<int>(blockIdx.y) * kMergeWarps + warp;
+    const int unit = static_cast<int>(blockIdx.x) / p.row_groups, quad = static_cast<int>(blockIdx.y);
+    const int row = ((static_cast<int>(blockIdx.x) - unit * p.row_groups) * kMergeWarps + warp) * kWarpRows + lane % kWarpRows;
+    const int b = unit / p.Hkv, kvh = unit - b * p.Hkv, tile = row / kTileRows, r = row % kTileRows;
+    // (the plan is not new any more: the kernel before has waited for it before it let this one start)
+    const int2 head = p.heads ? __ldcg(p.heads + unit) : make_int2(unit * p.n_splits, p.n_splits);      // first slot, parts
     pdl_trigger();
     pdl_wait();                                             // the partial results come from the previous kernel
-    const int2 head = p.heads ? __ldcg(p.heads + b) : make_int2(0, p.n_splits);      // first CTA, splits
-    const int n = __ldcg(p.tail_len + b) < 0 ? 0 : p.n_new ? min(__ldcg(p.n_new + b), p.n_max) : p.n_max;
-    const int row = rows0 + lane;
-    if (head.y < 2 || rows0 >= n << lr) return;
-    const bool on = row < n << lr;
-    const int r = row % kTileRows;
-    const long long cta0 = head.x + static_cast<long long>(kvh) * head.y * p.row_tiles + tile;
-    constexpr int kAhead = kDeep ? 6 : 4, kEvery = kDeep ? kMergeWarps : 1;
+    if (head.y < 2 || tile >= p.row_tiles) return;          // (the same for the whole warp: it has rows of one tile)
+    const int len = __ldcg(p.tail_len + b), n_new = p.n_new ? __ldcg(p.n_new + b) : p.n_max;
+    const long long slot0 = static_cast<long long>(head.x) * p.row_tiles + tile;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float m = kNegInf, l = 0.f;
-    for (int s0 = kDeep ? warp : 0; s0 < head.y && on; s0 += kAhead * kEvery) {
+    for (int s0 = of; s0 < head.y; s0 += kAhead * kLanes) {
         float lse[kAhead];
         float4 x[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int s = s0 + u * kEvery;
+            const int s = s0 + u * kLanes;
             lse[u] = kNegInf;
             if (s < head.y) {
-                const long long cta = cta0 + static_cast<long long>(s) * p.row_tiles;
-                lse[u] = __ldcg(p.part_lse + cta * kTileRows + r);
-                x[u] = __ldcg(reinterpret_cast<const float4 *>(p.part_o) + (cta * (D / 4) + quad) * kTileRows + r);
+                const long long slot = slot0 + static_cast<long long>(s) * p.row_tiles;
+                lse[u] = __ldcg(p.part_lse + slot * kTileRows + r);
+                x[u] = __ldcg(reinterpret_cast<const float4 *>(p.part_o) + (slot * (D / 4) + quad) * kTileRows + r);
             }
         }
         float m_new = m;
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) m_new = fmaxf(m_new, lse[u]);
-        if (m_new == kNegInf) continue;                     // splits that saw no key
+        if (m_new == kNegInf) continue;                     // parts that saw no key
         const float alpha = ex2(m - m_new);
         l *= alpha;
         acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
@@ -518,27 +603,18 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 8) tree_merge_kernel(const _
             acc.z = fmaf(f, x[u].z, acc.z); acc.w = fmaf(f, x[u].w, acc.w);
         }
     }
-    if (kDeep) {
-        sums[warp][lane] = acc;
-        refs[warp][lane] = make_float2(m, l);
-        __syncthreads();
-        if (warp != 0) return;
-        float top = kNegInf;
+    // the lanes of a row, in a fixed order
 #pragma unroll
-        for (int g = 0; g < kMergeWarps; ++g) top = fmaxf(top, refs[g][lane].x);
-        acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        l = 0.f;
-#pragma unroll
-        for (int g = 0; g < kMergeWarps; ++g) {
-            const float2 ml = refs[g][lane];
-            if (ml.x == kNegInf) continue;
-            const float f = ex2(ml.x - top);
-            const float4 x = sums[g][lane];
-            l = fmaf(f, ml.y, l);
-            acc.x = fmaf(f, x.x, acc.x); acc.y = fmaf(f, x.y, acc.y); acc.z = fmaf(f, x.z, acc.z); acc.w = fmaf(f, x.w, acc.w);
-        }
+    for (int o = kWarpRows; o < 32; o <<= 1) {
+        const float m2 = __shfl_xor_sync(kFull, m, o), l2 = __shfl_xor_sync(kFull, l, o);
+        const float4 x = make_float4(__shfl_xor_sync(kFull, acc.x, o), __shfl_xor_sync(kFull, acc.y, o), __shfl_xor_sync(kFull, acc.z, o), __shfl_xor_sync(kFull, acc.w, o));
+        const float top = fmaxf(m, m2), a = m == kNegInf ? 0.f : ex2(m - top), c = m2 == kNegInf ? 0.f : ex2(m2 - top);
+        l = l * a + l2 * c;
+        acc.x = acc.x * a + x.x * c; acc.y = acc.y * a + x.y * c; acc.z = acc.z * a + x.z * c; acc.w = acc.w * a + x.w * c;
+        m = top;
     }
-    if (!on) return;
+    const int n = len < 0 ? 0 : min(n_new, p.n_max);
+    if (of != 0 || row >= n << lr) return;
     const float inv = l > 0.f ? 1.f / l : 0.f;
     uint2 *dst = reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) +
                  ((static_cast<long long>(b) * p.n_max + (row >> lr)) * p.Hq + kvh * p.rep + (row & (p.rep - 1))) * D + quad * 4);
@@ -574,13 +650,19 @@ cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, bool deep, cudaStream_t st)
+template <int D>
+static cudaError_t launch_merge(TreeMergeParams p, int batch, int most, cudaStream_t st)
+{
+    // Few parts (calls with many units): lanes side by side; many: eight lanes a row, five parts each at a time.
+    const int lanes = most > 4 ? 8 : 1, rows = kMergeWarps * 32 / lanes;
+    p.row_groups = (p.n_max * p.rep + rows - 1) / rows;
+    const dim3 grid(static_cast<unsigned>(batch) * p.Hkv * p.row_groups, D / 4), block(kMergeWarps * 32);
+    return lanes == 8 ? launch_pdl(tree_merge_kernel<D, 8, 5>, grid, block, 0, st, p) : launch_pdl(tree_merge_kernel<D, 1, 4>, grid, block, 0, st, p);
+}
+cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, int most, cudaStream_t st)
 {
     if (head_dim != 128 && head_dim != 64) return cudaErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(batch) * p.Hkv * p.row_groups, deep ? head_dim / 4 : head_dim / (4 * kMergeWarps)), block(kMergeWarps * 32);
-    const auto kernel = head_dim == 128 ? (deep ? tree_merge_kernel<128, true> : tree_merge_kernel<128, false>)
-                                        : (deep ? tree_merge_kernel<64, true> : tree_merge_kernel<64, false>);
-    const cudaError_t e = launch_pdl(kernel, grid, block, 0, st, p);
+    const cudaError_t e = head_dim == 128 ? launch_merge<128>(p, batch, most, st) : launch_merge<64>(p, batch, most, st);
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -154,6 +154,29 @@ def test_one_long_request_among_short_ones():
     run((8, 2, 128), [[700] * 9, [20], [33], [16, 16]], [900, 3, 0, 17], [20, 20, 1, 7], 20)
 
 
+@pytest.mark.parametrize("model,batch,n_max", [((8, 2, 64), 64, 5), ((16, 2, 128), 60, 12), ((32, 2, 128), 40, 24), ((8, 2, 128), 62, 30)], ids=str)
+def test_runs_of_parts_across_requests(model, batch, n_max):
+    """Streams that do not divide into equal parts: most CTAs take the end of one and the beginning of the next, with other counts of rows; some
+    of them belong to requests that have ended or have no nodes, the first ones too."""
+    rng = np.random.default_rng(n_max)
+    tails, n_new = rng.integers(0, 300, batch), rng.integers(0, n_max + 1, batch)
+    tails[::9], n_new[3::8] = -1, 0
+    c = Case(model, [[int(rng.integers(500, 800)) for _ in range(4)] for _ in range(batch)], tails, n_new, n_max, seed=n_max)
+    try:
+        c.call()
+        tiles = -(-n_max * (model[0] // model[1]) // 128)
+        assert enl.enl_plan_inspect(c.cache)["n_items"] == 296 // tiles * tiles, "equal parts: not what this test is for"
+        c.check()
+        first = c.out.clone()
+        for _ in range(3):
+            c.out[:] = 7.0
+            c.call()
+            torch.cuda.synchronize()
+            assert torch.equal(first, c.out)
+    finally:
+        c.close()
+
+
 @pytest.mark.parametrize("model,nodes", [((32, 8, 128), 1), ((32, 8, 128), 30), ((32, 8, 128), 64), ((16, 2, 128), 40), ((32, 2, 128), 64), ((16, 1, 64), 64),
                                          ((8, 8, 64), 64)], ids=str)
 def test_long_streams(model, nodes):

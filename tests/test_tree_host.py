@@ -232,6 +232,51 @@ def test_grid_and_splits(host):
     assert host.fake_grid() <= 296 and host.fake_grid() % 8 == 0 and host.fake_splits() > 4
 
 
+@pytest.mark.parametrize("batch,lens,blocks,n_max,kv", [(16, (180, 230), 52, 24, 8), (16, (180, 230), 52, 64, 8), (3, (1100, 1500), 40, 16, 8), (40, (70, 140), 30, 8, 8),
+                                                        (64, (40, 90), 20, 1, 8), (5, (600, 1000), 3, 33, 2)], ids=str)
+def test_shares_of_several_requests(host, batch, lens, blocks, n_max, kv):
+    """Every unit's parts meet from its beginning to its end and have slots and heads of their own, a run is about as long as any other,
+    and CTAs find a place each."""
+    rng = np.random.default_rng(batch)
+    pages = rng.integers(lens[0], lens[1], batch)
+    d = dict(max_groups=batch, max_tokens=int(pages.sum()) * 16 + 16 * batch, max_batch=64, n_q_heads=4 * kv, n_kv_heads=kv)
+    c = Host.__new__(Host)
+    desc = enl.CacheDesc(1, 32, 8, 128, 0, 8, 4096, enl.ENL_BF16, 0, 4, 0, 0)
+    for k, v in d.items():
+        setattr(desc, k, v)
+    c.L, c.h = host, ctypes.c_void_p()
+    assert host.enl_cache_create(ctypes.byref(desc), ctypes.byref(c.h)) == enl.ENL_OK
+    for g in range(batch):
+        c.store(g, 0, int(pages[g]) * 16)
+    c.kinds()
+    assert c.call(sel=np.arange(batch, dtype=np.int32), batch=batch, cu_sel=np.arange(batch + 1, dtype=np.int32), n_max=n_max, max_blocks=blocks) == enl.ENL_OK
+    assert c.kinds()[0] == "p"                                    # a large plan: copied, so that it can be read here
+    tiles = -(-n_max * 4 // 128)
+    groups, off = host.fake_groups(), [host.fake_segment_off(i) for i in range(host.fake_groups() + 1)]
+    assert off[0] == 0 and all(a < b for a, b in zip(off, off[1:])) and host.fake_grid() == groups * tiles
+    seg = [[host.fake_segment(i, f) for f in range(7)] for i in range(off[-1])]
+    units, slots, at = {}, set(), np.concatenate([[0], np.cumsum(-(-pages // 8) * 8)])
+    for head, slot, first, count, a, b, whole in seg:
+        units.setdefault((head >> 16, head & 0xffff), []).append((a, b, whole, slot, first, count))
+        if slot >= 0:
+            assert slot not in slots
+            slots.add(slot)
+    assert sorted(units) == [(r, h) for r in range(batch) for h in range(kv)] and slots == set(range(len(slots)))
+    for (r, h), parts in units.items():
+        assert parts[0][0] == 0 and parts[-1][1] == parts[-1][2] and all(x[1] == y[0] and x[2] == y[2] for x, y in zip(parts, parts[1:]))
+        assert parts[0][4] == at[r] and sum(x[5] for x in parts) == pages[r] and all(x[4] + x[5] == y[4] for x, y in zip(parts, parts[1:]))
+        assert (len(parts) == 1) == (parts[0][3] < 0)
+        if len(parts) > 1:
+            assert [x[3] for x in parts] == list(range(parts[0][3], parts[0][3] + len(parts)))
+        if host.fake_splits() > 1:
+            assert host.fake_unit(r * kv + h, 1) == len(parts) and (len(parts) == 1 or host.fake_unit(r * kv + h, 0) == parts[0][3])
+    work = [sum((b - a) / whole * (pages[head >> 16] + blocks + -(-n_max // 16)) for head, _, _, _, a, b, whole in seg[i:j]) for i, j in zip(off, off[1:])]
+    units_per_place = batch * kv * tiles / 296
+    if units_per_place < 1:
+        assert groups * tiles <= 296
+        assert max(work) <= sum(work) / (296 // tiles) * 1.35 + 4 * 4, (max(work), sum(work) / (296 // tiles))
+
+
 # ---- the calls without a cache: nothing is followed before everything has been looked at ---------------------------------------
 def filled(cls, **kw):
     a = cls()
