@@ -202,6 +202,7 @@ struct TreeParams {
     int32_t box_tokens;     // tokens of a Q box
     int32_t n_splits, n_entries;    // of a single request
     int32_t wait_first;     // as in AttnParams
+    int32_t early_steps;    // most steps that are fetched before the wait for the previous kernel
     float   scale_log2;
 };
 struct TreeMergeParams {

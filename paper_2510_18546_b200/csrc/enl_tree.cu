@@ -12,6 +12,7 @@ namespace {
 
 constexpr int kStepPages = kStepKeys / kPageTokens;
 constexpr int kMergeSteps = 4;      // what putting parts together costs, in steps of a CTA
+constexpr int kEarly = 8, kEarlyMerge = 2;      // steps fetched before the wait for the previous kernel; where that is a merge kernel, whose loads they hold up
 constexpr int kSegmentSteps = 2;    // what another segment of a CTA costs
 
 int64_t steps_of(int64_t pages) { return (pages + kStepPages - 1) / kStepPages; }
@@ -140,9 +141,9 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         if (n_entries > c->cap_entries) return ENL_E_NOMEM;
 
         // Shares of the CTAs.  The host does not know how long the tails are, so they count for what their tables hold: too many parts of a stream
-        // that turns out short cost little, since all CTAs run at once.  Two of them fit a multiprocessor.
+        // that turns out short cost little, since all CTAs run at once, one on a multiprocessor.
         const int64_t slot_bytes = static_cast<int64_t>(kTileRows) * (d.head_dim + 1) * 4 * row_tiles;
-        const int64_t places = std::max<int64_t>(1, 2 * c->n_sm / row_tiles), slots = d.scratch_bytes / slot_bytes;
+        const int64_t places = std::max<int64_t>(1, c->n_sm / row_tiles), slots = d.scratch_bytes / slot_bytes;
         std::vector<int64_t> pages(B), parts(B, 1);
         for (int b = 0; b < B; ++b) {
             pages[b] = ceil_div(a->n_max, kPageTokens) + static_cast<int64_t>(a->max_blocks);
@@ -275,6 +276,7 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
     p.row_tiles = row_tiles;
     p.n_splits = c->plan_splits;
     p.n_entries = c->tree_entries;
+    p.early_steps = c->plan_splits > 1 ? kEarlyMerge : kEarly;
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(d.head_dim));
 
     p.part_o = c->scratch;

@@ -9,16 +9,20 @@
 //   S = Q K^T               tcgen05.mma into one of two TMEM buffers of 64 columns
 //   p = exp2(S * c - m)     one thread per row, hidden keys -inf before the maximum
 //   O += P V                tcgen05.mma, P (bf16) out of the TMEM columns that held the scores
-// Roles: a softmax warp per 32 rows, a warp that fetches K, one that fetches V, one that issues the MMAs and owns the TMEM.
+// Two walkers (a softmax warpgroup and a warp that issues its MMAs) take the steps in turns, each with an accumulator of its own, and put
+// them together at the end, in TMEM lanes that both read.  Warps: 0-3 and 4-7 softmax of walker 0 and 1, 8 fetches K, 10 fetches V, 9 and
+// 11 issue the MMAs (9 owns the TMEM).
 //
 // What bounds it: a tree has few rows, so the keys' bytes do (64 keys of a kv head are 32 KB, which take a multiprocessor some 1400 cycles
-// of its share of the memory; the tensor pipe needs 512 of them and the special-function units 512).  Hence two CTAs per
-// multiprocessor, whose chains scores -> softmax -> P V overlap, and splits that fill the device whatever the batch.
+// of its share of the memory; the tensor pipe needs 512 of them and the special-function units 512, but a walker's chain
+// scores -> softmax -> P V is 1600 long).  Hence two walkers, and shares that fill the device whatever the batch.  (Two CTAs per
+// multiprocessor with one walker each left twice as many partial results.)
 //
 // Shares: the host knows the cached pages of a request, but not how long its tail is.  So it cuts the stream of a request and kv head (a "unit")
 // by fractions: the part from a / E to b / E takes those pages of the C cached ones and the same part of the tail's and the nodes' pages, whose
 // number the device finds.  A CTA has one part, or, where the units do not divide into equal parts (see enl_tree.cu), a run of parts of
-// consecutive units that is as long as any other CTA's; the loads of a part run under the one before it.  The cached pages of the first steps are fetched before the
+// consecutive units that is as long as any other CTA's; the loads of a part run under the one before it, and the producer of K leaves what
+// the other warps have to know of it in shared memory.  The cached pages of the first steps are fetched before the
 // kernel waits for the one before it (plan and pool are written by the library only).
 // Parts of a unit leave outputs normalised by their own sums, and log2-sum-exps, in the scratch buffer; tree_merge_kernel puts them together.
 #include <cuda_bf16.h>
@@ -30,57 +34,74 @@
 namespace enl {
 namespace {
 
-constexpr uint32_t kTmemCols = 256;           // two CTAs per multiprocessor
-constexpr uint32_t kOCol = 128;               // S: [0, 64) and [64, 128), O: [128, 128 + D)
+constexpr int kThreads = 384;
+constexpr int kKWarp = 8, kMmaWarp = 9, kVWarp = 10;         // (the MMAs of walker 1: two warps on)
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kOCol = 256;               // S of walker i: 128 i + two buffers of 64 columns, O: 256 + 128 i
 constexpr int kStepPages = kStepKeys / kPageTokens;
 constexpr int kBatch = 32 / kStepPages;       // steps whose pages a warp's lanes hold, one each
 constexpr float kRescaleThreshold = 8.0f;     // log2 units: p stays below 2^8 between updates of the reference
 
-// kRows: 64 or 128 query rows.  The Q tile of 64 rows is half of what the MMA reads: the other rows of its operand are whatever lies behind it
-// (the next block of channels, the ring), and their results are not looked at.  The 16 KB go to the ring.
-template <int D, int kRows>
+template <int D>
 struct Cfg {
-    static constexpr int kSoftmaxWarps = kRows / 32, kKWarp = kSoftmaxWarps, kVWarp = kKWarp + 1, kMmaWarp = kKWarp + 2;
-    static constexpr int kThreads    = (kSoftmaxWarps + 3) * 32;
     static constexpr int kBlocks     = D / 64;                // 64-channel (128-byte) column blocks
-    static constexpr int kBlockBytes = kRows * 128;           // of the Q tile
+    static constexpr int kBlockBytes = kTileRows * 128;       // of the Q tile
     static constexpr int kTileBytes  = kBlocks * kBlockBytes;
     static constexpr int kGroupBytes = kBlocks * 1024;        // eight rows of K or V
     static constexpr int kStepBytes  = kStepKeys / 8 * kGroupBytes;
-    // steps whose K, and whose V, are in shared memory at once: all that two CTAs have room for (V stays until its step's softmax is done)
-    static constexpr int kRingK      = D == 64 ? 6 : kRows == 64 ? 3 : 2;
-    static constexpr int kRingV      = D == 64 ? 6 : 3;
+    // Steps whose K, and whose V, are in shared memory at once (V stays until its step's softmax is done).  Even numbers: a place belongs to one
+    // walker, whose waits for it then follow one another.
+    static constexpr int kRingK      = D == 64 ? 8 : 4;
+    static constexpr int kRingV      = D == 64 ? 8 : 6;
+    static_assert(kRingK % 2 == 0 && kRingV % 2 == 0, "a place, a walker");
+    static constexpr int kEarly      = kRingK < kRingV ? kRingK : kRingV;
     static constexpr int kKOff       = kTileBytes;
     static constexpr int kVOff       = kKOff + kRingK * kStepBytes;
-    static constexpr int kBarOff     = kVOff + kRingV * kStepBytes;
-    static constexpr int kBars       = 9 + 2 * (kRingK + kRingV);
+    static constexpr int kMlOff      = kVOff + kRingV * kStepBytes;      // [walker][row] reference and sum
+    static constexpr int kInfoOff    = kMlOff + 2 * kTileRows * 8;       // what the warps have to know of a segment, [2]
+    static constexpr int kBarOff     = kInfoOff + 2 * 64;
+    static constexpr int kBars       = 15 + 2 * (kRingK + kRingV);
     static constexpr int kSmemBytes  = kBarOff + 8 * kBars + 8;
-    static_assert(kSmemBytes <= 115712, "two CTAs per multiprocessor");
+    static_assert(kSmemBytes <= 232448 - 2048, "a CTA of the merge kernel beside it");
 };
 
 __device__ __forceinline__ int pages_of(int rows) { return (rows + kPageTokens - 1) / kPageTokens; }
 
-template <int D, int kRows>
-__global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __grid_constant__ TreeParams p)
+// A segment as the warps behind the producers need it.
+struct Info {
+    int b, kvh, slot;                         // request, kv head, slot of the partial results (-1: the whole)
+    int first, count;                         // stream entries (cached pages)
+    int t_first, t_count;                     // pages of the tail, and of the nodes behind it
+    int tail_pages, len, n;                   // pages and rows of the whole tail, nodes
+    int n_steps;
+    int more;                                 // another segment follows
+};
+static_assert(sizeof(Info) <= 64, "shared memory");
+
+// (384 threads may have 168 registers; 144 leave room for a CTA of the merge kernel)
+template <int D>
+__global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams p)
 {
-    using C = Cfg<D, kRows>;
+    using C = Cfg<D>;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     const uint32_t bar0 = sbase + C::kBarOff;
-    const uint32_t bar_q_full = bar0, bar_q_empty = bar0 + 8u;                   // the Q tile of a segment is there / may be overwritten
-    const uint32_t bar_pv_done = bar0 + 16u, bar_o_done = bar0 + 24u;           // P V of a step / of a segment's last one
-    const uint32_t bar_o_free = bar0 + 32u;                                     // the accumulator has been read
-    auto bar_s_full  = [&](int b) { return bar0 + 8u * (5 + b); };              // b: step & 1
-    auto bar_p_full  = [&](int b) { return bar0 + 8u * (7 + b); };
-    auto bar_k_full  = [&](int x) { return bar0 + 8u * (9 + x); };              // x: place in the ring
-    auto bar_k_empty = [&](int x) { return bar0 + 8u * (9 + C::kRingK + x); };
-    auto bar_v_full  = [&](int x) { return bar0 + 8u * (9 + 2 * C::kRingK + x); };
-    auto bar_v_empty = [&](int x) { return bar0 + 8u * (9 + 2 * C::kRingK + C::kRingV + x); };
+    const uint32_t bar_q_full = bar0, bar_q_empty = bar0 + 8u;                   // a segment's Q tile and Info are there / may be overwritten
+    const uint32_t bar_o_free = bar0 + 16u;                                     // the accumulators have been read
+    auto bar_pv_done = [&](int i) { return bar0 + 8u * (3 + i); };              // P V of a step of walker i / of its last one of a segment
+    auto bar_o_done  = [&](int i) { return bar0 + 8u * (5 + i); };
+    auto bar_s_full  = [&](int i, int b) { return bar0 + 8u * (7 + 2 * i + b); };      // b: step & 1 (of the walker's steps)
+    auto bar_p_full  = [&](int i, int b) { return bar0 + 8u * (11 + 2 * i + b); };
+    auto bar_k_full  = [&](int x) { return bar0 + 8u * (15 + x); };             // x: place in the ring
+    auto bar_k_empty = [&](int x) { return bar0 + 8u * (15 + C::kRingK + x); };
+    auto bar_v_full  = [&](int x) { return bar0 + 8u * (15 + 2 * C::kRingK + x); };
+    auto bar_v_empty = [&](int x) { return bar0 + 8u * (15 + 2 * C::kRingK + C::kRingV + x); };
     auto phase_of = [](int at, int places) { return static_cast<uint32_t>((at / places) & 1); };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kBarOff + 8 * C::kBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    Info *infos = reinterpret_cast<Info *>(smem + C::kInfoOff);
 
     if (sbase & 1023u) {                      // (swizzled tiles need it, and dynamic shared memory starts like this)
         if (threadIdx.x == 0) atomicExch(p.status, 1);
@@ -90,49 +111,26 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
     // ---- what this CTA does: a tile of rows of its segments (see TreeSegment) ----
     const int group = p.row_tiles == 1 ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) / p.row_tiles;
     const int rt = p.row_tiles == 1 ? 0 : static_cast<int>(blockIdx.x) - group * p.row_tiles;
-    struct Part { int b, kvh, slot, first, count, from, to, whole; };
-    auto segment = [&](int i) -> Part {
-        Part w;
-        if (p.batch == 1) {
-            w.b = 0;
-            w.kvh = group / p.n_splits;
-            w.from = group - w.kvh * p.n_splits;
-            w.to = w.from + 1;
-            w.whole = p.n_splits;
-            w.slot = p.n_splits > 1 ? group : -1;
-            w.first = static_cast<int>(static_cast<long long>(p.n_entries) * w.from / p.n_splits);
-            w.count = static_cast<int>(static_cast<long long>(p.n_entries) * w.to / p.n_splits) - w.first;
-        } else {
-            const int4 *src = reinterpret_cast<const int4 *>(p.segments + i);
-            const int4 x = __ldcg(src), y = __ldcg(src + 1);
-            w.b = x.x >> 16; w.kvh = x.x & 0xffff; w.slot = x.y; w.first = x.z; w.count = x.w;
-            w.from = y.x; w.to = y.y; w.whole = y.z;
-        }
-        return w;
-    };
-    int seg_beg = 0, seg_end = 1;
-    if (p.batch > 1) {
-        seg_beg = __ldcg(p.segment_off + group);
-        seg_end = __ldcg(p.segment_off + group + 1);
-    }
-    Part it = segment(seg_beg);
+    const int rows_before = rt * kTileRows;
 
     // ---- set-up ----
-    if (warp == C::kMmaWarp) {
+    if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                      ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     if (threadIdx.x == 0) {
         *abort_flag = 0;
-        mbar_init(bar_q_full, 1);
-        mbar_init(bar_q_empty, 1);
-        mbar_init(bar_o_free, C::kSoftmaxWarps);                  // (with rows or without)
-        mbar_init(bar_pv_done, 1);
-        mbar_init(bar_o_done, 1);
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(bar_s_full(b), 1);
-            mbar_init(bar_p_full(b), C::kSoftmaxWarps);           // (the first warp arrives for those without rows, too)
+        mbar_init(bar_q_full, 2);                                 // the Q tile, the Info
+        mbar_init(bar_q_empty, 2 + 8);                            // both walkers' last Q K^T, every softmax warp's look at the Info
+        mbar_init(bar_o_free, 8);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar_pv_done(i), 1);
+            mbar_init(bar_o_done(i), 1);
+            for (int b = 0; b < 2; ++b) {
+                mbar_init(bar_s_full(i, b), 1);
+                mbar_init(bar_p_full(i, b), 4);                   // (a walker's first warp arrives for those without rows, too)
+            }
         }
         for (int x = 0; x < C::kRingK; ++x) { mbar_init(bar_k_full(x), 1); mbar_init(bar_k_empty(x), 1); }
         for (int x = 0; x < C::kRingV; ++x) { mbar_init(bar_v_full(x), 1); mbar_init(bar_v_empty(x), 1); }
@@ -145,33 +143,59 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
     pdl_trigger();
     bool ok = true;
 
-    // ---- lengths: a request that has ended, or has no nodes, leaves nothing to do; a tail is as long as its block table at most.  What comes from
-    // the kernel before is read past the L1, since this one may have started while that one ran. ----
-    int len = 0, n = 0, t_first = 0, t_count = 0, tail_pages = 0, n_steps = 0;
-    auto read_lengths = [&]() {
-        const int l0 = __ldcg(p.tail_len + it.b), n0 = p.n_new ? __ldcg(p.n_new + it.b) : p.n_max;
-        len = max(0, min(l0, p.max_blocks * kPageTokens));
-        n = l0 < 0 ? 0 : max(0, min(n0, p.n_max));
-        tail_pages = pages_of(len);
-        const int t = tail_pages + pages_of(n);
-        // (rising in `at`, 0 at 0 and t at the end: the parts of a unit meet)
-        auto cut = [&](int at) { return at >= it.whole ? t : min(t, static_cast<int>(static_cast<float>(t) * (static_cast<float>(at) / static_cast<float>(it.whole)))); };
-        t_first = cut(it.from);
-        t_count = cut(it.to) - t_first;
-        n_steps = rt * kRows < n * p.rep ? (it.count + t_count + kStepPages - 1) / kStepPages : 0;
-    };
-    // The steps of cached pages alone that the ring has room for are fetched before the wait for the kernel before.  A first segment that turns
-    // out to have no rows leaves them, and its Q tile, to be passed over.
-    const int early_k = p.wait_first ? 0 : min(C::kRingK, it.count / kStepPages), early_v = p.wait_first ? 0 : min(C::kRingV, it.count / kStepPages);
+    // steps that are fetched before the wait for the kernel before, of a first segment of `count` cached pages
+    auto early_of = [&](int count) { return p.wait_first ? 0 : min(min(C::kEarly, p.early_steps), count / kStepPages); };
 
-    if (warp == C::kKWarp || warp == C::kVWarp) {
+    if (warp == kKWarp || warp == kVWarp) {
         // ================= TMA producers =================
-        const bool is_k = warp == C::kKWarp;
+        const bool is_k = warp == kKWarp;
         const CUtensorMap *tm_pool = is_k ? &p.tm_kpool : &p.tm_vpool, *tm_tail = is_k ? &p.tm_ktail : &p.tm_vtail,
                           *tm_new = is_k ? &p.tm_knew : &p.tm_vnew;
         const uint32_t ring = sbase + static_cast<uint32_t>(is_k ? C::kKOff : C::kVOff), full0 = is_k ? bar_k_full(0) : bar_v_full(0),
                        empty0 = is_k ? bar_k_empty(0) : bar_v_empty(0);
-        const int places = is_k ? C::kRingK : C::kRingV, early = is_k ? early_k : early_v;
+        const int places = is_k ? C::kRingK : C::kRingV;
+        struct Part { int b, kvh, slot, first, count, from, to, whole; };
+        auto segment = [&](int i) -> Part {
+            Part w;
+            if (p.batch == 1) {
+                w.b = 0;
+                w.kvh = group / p.n_splits;
+                w.from = group - w.kvh * p.n_splits;
+                w.to = w.from + 1;
+                w.whole = p.n_splits;
+                w.slot = p.n_splits > 1 ? group : -1;
+                w.first = static_cast<int>(static_cast<long long>(p.n_entries) * w.from / p.n_splits);
+                w.count = static_cast<int>(static_cast<long long>(p.n_entries) * w.to / p.n_splits) - w.first;
+            } else {
+                const int4 *src = reinterpret_cast<const int4 *>(p.segments + i);
+                const int4 x = __ldcg(src), y = __ldcg(src + 1);
+                w.b = x.x >> 16; w.kvh = x.x & 0xffff; w.slot = x.y; w.first = x.z; w.count = x.w;
+                w.from = y.x; w.to = y.y; w.whole = y.z;
+            }
+            return w;
+        };
+        int seg_beg = 0, seg_end = 1;
+        if (p.batch > 1) {
+            seg_beg = __ldcg(p.segment_off + group);
+            seg_end = __ldcg(p.segment_off + group + 1);
+        }
+        // Lengths: a request that has ended, or has no nodes, leaves nothing to do; a tail is as long as its block table at most.  What comes from
+        // the kernel before is read past the L1, since this one may have started while that one ran.
+        Part it = segment(seg_beg), ahead = it;                      // this segment, and the next one, fetched a segment ahead
+        int2 raw = make_int2(0, 0), raw_ahead = raw;                                         // rows of the tail and nodes, as they are in memory
+        auto lengths = [&](int b) { return make_int2(__ldcg(p.tail_len + b), p.n_new ? __ldcg(p.n_new + b) : p.n_max); };
+        int len = 0, n = 0, t_first = 0, t_count = 0, tail_pages = 0, n_steps = 0;
+        auto take_lengths = [&]() {
+            len = max(0, min(raw.x, p.max_blocks * kPageTokens));
+            n = raw.x < 0 ? 0 : max(0, min(raw.y, p.n_max));
+            tail_pages = pages_of(len);
+            const int t = tail_pages + pages_of(n);
+            // (rising in `at`, 0 at 0 and t at the end: the parts of a unit meet)
+            auto cut = [&](int at) { return at >= it.whole ? t : min(t, static_cast<int>(static_cast<float>(t) * (static_cast<float>(at) / static_cast<float>(it.whole)))); };
+            t_first = cut(it.from);
+            t_count = cut(it.to) - t_first;
+            n_steps = rows_before < n * p.rep ? (it.count + t_count + kStepPages - 1) / kStepPages : 0;
+        };
         // Where pages lie, one per lane, fetched eight steps ahead: kind << 30 | page of the pool (0), of the tail (1), first row among the
         // request's nodes (2).  What fills the last step, and an entry of the block table that names no page, is the page of zeros.
         auto where = [&](int i) -> uint32_t {
@@ -201,33 +225,48 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
             }
         };
         auto fetch_q = [&]() {
-            if (is_k && lane == 0) {
+            if (lane == 0) {
                 mbar_expect_tx(bar_q_full, static_cast<uint32_t>(C::kBlocks * p.box_tokens * p.rep * 128));
                 for (int b = 0; b < C::kBlocks; ++b)
-                    tma_load_3d(sbase + b * C::kBlockBytes, &p.tm_q, b * 64, it.kvh * p.rep, it.b * p.n_max + rt * (kRows / p.rep), bar_q_full);
+                    tma_load_3d(sbase + b * C::kBlockBytes, &p.tm_q, b * 64, it.kvh * p.rep, it.b * p.n_max + rt * (kTileRows / p.rep), bar_q_full);
             }
             __syncwarp();
         };
-        static_assert(C::kRingK < kBatch && C::kRingV < kBatch, "the early steps' pages are of one batch");
+        auto announce = [&](int si) {
+            if (lane == 0) {
+                infos[(si - seg_beg) & 1] = Info{it.b, it.kvh, it.slot, it.first, it.count, t_first, t_count, tail_pages, len, n, n_steps, si + 1 < seg_end};
+                mbar_arrive(bar_q_full);
+            }
+            __syncwarp();
+        };
+        // The steps of cached pages alone that the ring has room for are fetched before the wait for the kernel before.  (A first segment that turns
+        // out to have no rows leaves them, and its Q tile, to be passed over.)
+        static_assert(C::kRingK <= kBatch && C::kRingV <= kBatch, "the early steps' pages are of one batch");
+        const int early = early_of(it.count);
         uint32_t cur = 0, next = where(lane);                        // (of the cached pages so far)
-        int f = 0, qn = 1;                                           // steps fetched, Q tiles fetched
+        int f = 0;                                                   // steps fetched
         for (; f < early; ++f) fetch(__shfl_sync(kFull, next, f * kStepPages + lane % kStepPages), f);
         pdl_wait();
-        fetch_q();
-        read_lengths();
+        if (is_k) fetch_q();
+        raw = raw_ahead = lengths(it.b);
+        if (seg_beg + 1 < seg_end) {
+            ahead = segment(seg_beg + 1);
+            raw_ahead = lengths(ahead.b);
+        }
+        take_lengths();
+        if (is_k) announce(seg_beg);
         for (int si = seg_beg; ok;) {
             int jj = si == seg_beg && n_steps > 0 ? early : 0;
-            if (si > seg_beg) {
-                next = where(lane);
-                if (is_k && n_steps > 0) {
-                    ok = mbar_wait(bar_q_empty, static_cast<uint32_t>((qn - 1) & 1), abort_flag, p.status);
-                    if (!ok) break;
-                    fetch_q();
-                    ++qn;
-                }
-            } else if (lane >= it.count) {
-                next = where(lane);
-            }
+            bool q_due = is_k && si > seg_beg;                       // Q tile and Info of a later segment, as soon as those before have been used
+            auto follow = [&]() {
+                ok = mbar_wait(bar_q_empty, static_cast<uint32_t>((si - seg_beg - 1) & 1), abort_flag, p.status);
+                if (!ok) return;
+                if (n_steps > 0) fetch_q();
+                else if (lane == 0) mbar_arrive(bar_q_full);
+                announce(si);
+                q_due = false;
+            };
+            if (si > seg_beg || lane >= it.count) next = where(lane);
             cur = next;
             if (jj > 0) next = where(kBatch * kStepPages + lane);
             for (; jj < n_steps; ++jj) {
@@ -236,15 +275,22 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                     cur = next;
                     next = where((jj + kBatch) * kStepPages + lane);
                 }
+                if (q_due && (jj == places || __any_sync(kFull, mbar_test(bar_q_empty, static_cast<uint32_t>((si - seg_beg - 1) & 1))))) follow();
                 const uint32_t at = __shfl_sync(kFull, cur, jj % kBatch * kStepPages + lane % kStepPages);
-                if (f >= places) ok = mbar_wait(empty0 + 8u * x, phase_of(f, places) ^ 1u, abort_flag, p.status);
+                if (ok && f >= places) ok = mbar_wait(empty0 + 8u * x, phase_of(f, places) ^ 1u, abort_flag, p.status);
                 if (!ok) break;
                 fetch(at, x);
                 ++f;
             }
+            if (ok && q_due) follow();
             if (++si >= seg_end) break;
-            it = segment(si);
-            read_lengths();
+            it = ahead;
+            raw = raw_ahead;
+            if (si + 1 < seg_end) {
+                ahead = segment(si + 1);
+                raw_ahead = lengths(ahead.b);
+            }
+            take_lengths();
         }
         // error path only: copies in flight land before the CTA retires
         if (!ok) {
@@ -253,104 +299,114 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                 while (!mbar_try_wait(full0 + 8u * (e % places), phase_of(e, places)) && global_ns() - t0 < 2000000ull) { }
             }
         }
-    } else if (warp == C::kMmaWarp) {
-        // ================= MMA issuer =================
+    } else if (warp >= 8) {
+        // ================= MMA issuer of a walker =================
+        const int i = warp == kMmaWarp ? 0 : 1;
         pdl_wait();
-        read_lengths();
         constexpr uint32_t idesc_qk = make_idesc(kStepKeys, false), idesc_pv = make_idesc(D, true);
         constexpr uint32_t kStepUnits = C::kStepBytes >> 4, kGroupUnits = C::kGroupBytes >> 4;
         const uint64_t dq0 = smem_desc(sbase, 16), dk0 = smem_desc(sbase + C::kKOff, 16, C::kGroupBytes), dv0 = smem_desc(sbase + C::kVOff, 1024, C::kGroupBytes);
         const uint32_t dq_lo = static_cast<uint32_t>(dq0), dq_hi = static_cast<uint32_t>(dq0 >> 32);
         const uint32_t dk_lo = static_cast<uint32_t>(dk0), dk_hi = static_cast<uint32_t>(dk0 >> 32);
         const uint32_t dv_lo = static_cast<uint32_t>(dv0), dv_hi = static_cast<uint32_t>(dv0 >> 32);
-        int fk = 0, fv = 0, g = 0, qn = 0, on = 0;                  // steps whose K, whose V has been used, steps, Q tiles and accumulators so far
-        auto issue_qk = [&](int at, bool last) {                     // step `at` of all
-            const int x = fk % C::kRingK, b = at & 1;
-            const uint32_t ka = dk_lo + static_cast<uint32_t>(x) * kStepUnits, d = tmem_base + static_cast<uint32_t>(b * kStepKeys);
+        const uint32_t t_s = tmem_base + static_cast<uint32_t>(i * 128), t_o = tmem_base + kOCol + static_cast<uint32_t>(i * 128);
+        // steps fetched for the segments before; this walker's steps, segments with a step of this walker, with a step at all so far
+        int f0 = 0, g = 0, on = 0, freed = 0, seg = 0;
+        auto issue_qk = [&](int f, int at, bool last) {              // the step that was fetched as number f, number `at` of this walker
+            const int x = f % C::kRingK, b = at & 1;
+            const uint32_t ka = dk_lo + static_cast<uint32_t>(x) * kStepUnits, d = t_s + static_cast<uint32_t>(b * kStepKeys);
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
                 const uint32_t in_row = static_cast<uint32_t>((kk & 3) * 2);                       // 32 bytes per 16 channels
                 mma_ss2(d, dq_lo + static_cast<uint32_t>((kk >> 2) * (C::kBlockBytes >> 4)) + in_row, dq_hi,
                         ka + static_cast<uint32_t>((kk >> 2) * (1024 >> 4)) + in_row, dk_hi, idesc_qk, kk > 0 ? 1u : 0u);
             }
-            tc_commit(bar_s_full(b));
+            tc_commit(bar_s_full(i, b));
             tc_commit(bar_k_empty(x));
             if (last) tc_commit(bar_q_empty);
-            ++fk;
         };
         // O (+)= P V; P of keys 2c, 2c + 1 sits in column c of the buffer that held their scores
-        auto issue_pv = [&](bool first, bool last) {
-            const int x = fv % C::kRingV, b = g & 1;
-            const uint32_t va = dv_lo + static_cast<uint32_t>(x) * kStepUnits, a = tmem_base + static_cast<uint32_t>(b * kStepKeys);
+        auto issue_pv = [&](int f, bool first, bool last) {
+            const int x = f % C::kRingV, b = g & 1;
+            const uint32_t va = dv_lo + static_cast<uint32_t>(x) * kStepUnits, a = t_s + static_cast<uint32_t>(b * kStepKeys);
 #pragma unroll
             for (int k4 = 0; k4 < kStepPages; ++k4)                  // 16 keys = two groups of 8 rows, 8 columns of P
-                mma_ts2(tmem_base + kOCol, a + static_cast<uint32_t>(k4 * 8), va + static_cast<uint32_t>(k4 * 2) * kGroupUnits, dv_hi, idesc_pv,
+                mma_ts2(t_o, a + static_cast<uint32_t>(k4 * 8), va + static_cast<uint32_t>(k4 * 2) * kGroupUnits, dv_hi, idesc_pv,
                         (first && k4 == 0) ? 0u : 1u);
             tc_commit(bar_v_empty(x));
-            tc_commit(last ? bar_o_done : bar_pv_done);
-            ++fv;
+            tc_commit(last ? bar_o_done(i) : bar_pv_done(i));
         };
-        auto wait_k = [&]() { return mbar_wait(bar_k_full(fk % C::kRingK), phase_of(fk, C::kRingK), abort_flag, p.status); };
-        auto wait_v = [&]() { return mbar_wait(bar_v_full(fv % C::kRingV), phase_of(fv, C::kRingV), abort_flag, p.status); };
-        for (int si = seg_beg; ok;) {
-            if (si == seg_beg || n_steps > 0) {
-                ok = mbar_wait(bar_q_full, static_cast<uint32_t>(qn & 1), abort_flag, p.status);
-                ++qn;
+        auto wait_k = [&](int f) { return mbar_wait(bar_k_full(f % C::kRingK), phase_of(f, C::kRingK), abort_flag, p.status); };
+        auto wait_v = [&](int f) { return mbar_wait(bar_v_full(f % C::kRingV), phase_of(f, C::kRingV), abort_flag, p.status); };
+        for (;; ++seg) {
+            ok = mbar_wait(bar_q_full, static_cast<uint32_t>(seg & 1), abort_flag, p.status);
+            if (!ok) break;
+            const volatile Info *info = infos + (seg & 1);
+            const int n_steps = info->n_steps, more_segments = info->more, passed = n_steps == 0 && seg == 0 ? early_of(info->count) : 0;
+            const int mine = (n_steps + 1 - i) >> 1;
+            for (int e = 0; i == 0 && e < passed && ok; ++e) {       // what was fetched for nothing
+                ok = wait_k(e) && wait_v(e);
+                if (lane == 0) {
+                    mbar_arrive(bar_k_empty(e));
+                    mbar_arrive(bar_v_empty(e));
+                }
             }
-            if (n_steps == 0 && si == seg_beg) {                     // what was fetched for nothing
-                for (int e = 0; e < early_k && ok; ++e, ++fk) {
-                    ok = wait_k();
-                    if (lane == 0) mbar_arrive(bar_k_empty(fk % C::kRingK));
-                }
-                for (int e = 0; e < early_v && ok; ++e, ++fv) {
-                    ok = wait_v();
-                    if (lane == 0) mbar_arrive(bar_v_empty(fv % C::kRingV));
-                }
+            if (mine == 0) {
+                __syncwarp();
                 if (lane == 0) mbar_arrive(bar_q_empty);
             }
-            for (int jj = 0; jj < min(2, n_steps) && ok; ++jj) {
-                ok = wait_k();
+            for (int jj = 0; jj < min(2, mine) && ok; ++jj) {
+                const int f = f0 + 2 * jj + i;
+                ok = wait_k(f);
                 if (!ok) break;
                 tc_fence_after();
-                issue_qk(g + jj, jj + 1 == n_steps);
+                issue_qk(f, g + jj, jj + 1 == mine);
             }
-            for (int jj = 0; jj < n_steps && ok; ++jj, ++g) {
-                const bool more = jj + 2 < n_steps;
-                ok = wait_v();
-                if (ok && more) ok = wait_k();
-                if (ok && jj == 0 && on > 0) ok = mbar_wait(bar_o_free, static_cast<uint32_t>((on - 1) & 1), abort_flag, p.status);
-                if (ok) ok = mbar_wait(bar_p_full(g & 1), static_cast<uint32_t>((g >> 1) & 1), abort_flag, p.status);
+            for (int jj = 0; jj < mine && ok; ++jj, ++g) {
+                const int f = f0 + 2 * jj + i;
+                const bool more = jj + 2 < mine;
+                ok = wait_v(f);
+                if (ok && more) ok = wait_k(f + 4);
+                if (ok && jj == 0 && freed > 0) ok = mbar_wait(bar_o_free, static_cast<uint32_t>((freed - 1) & 1), abort_flag, p.status);
+                if (ok) ok = mbar_wait(bar_p_full(i, g & 1), static_cast<uint32_t>((g >> 1) & 1), abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
-                issue_pv(jj == 0, jj + 1 == n_steps);
-                if (more) issue_qk(g + 2, jj + 3 == n_steps);
+                issue_pv(f, jj == 0, jj + 1 == mine);
+                if (more) issue_qk(f + 4, g + 2, jj + 3 == mine);
             }
-            if (n_steps > 0) ++on;
-            if (++si >= seg_end) break;
-            it = segment(si);
-            read_lengths();
+            if (!ok) break;
+            on += mine > 0 ? 1 : 0;
+            freed += n_steps > 0 ? 1 : 0;
+            f0 += n_steps + passed;
+            if (!more_segments) break;
         }
-        // nothing may arrive after the CTA has retired
-        for (int e = max(0, fk - C::kRingK); e < fk && ok; ++e) ok = mbar_wait(bar_k_empty(e % C::kRingK), phase_of(e, C::kRingK), abort_flag, p.status);
-        for (int e = max(0, fv - C::kRingV); e < fv && ok; ++e) ok = mbar_wait(bar_v_empty(e % C::kRingV), phase_of(e, C::kRingV), abort_flag, p.status);
-        if (ok) ok = mbar_wait(bar_q_empty, static_cast<uint32_t>((qn - 1) & 1), abort_flag, p.status);
-        if (ok && on > 0) ok = mbar_wait(bar_o_done, static_cast<uint32_t>((on - 1) & 1), abort_flag, p.status);
+        // nothing may arrive after the CTA has retired: the last use of every place, by either walker, and what counts segments
+        for (int e = max(0, f0 - C::kRingK); i == 0 && e < f0 && ok; ++e) ok = mbar_wait(bar_k_empty(e % C::kRingK), phase_of(e, C::kRingK), abort_flag, p.status);
+        for (int e = max(0, f0 - C::kRingV); i == 0 && e < f0 && ok; ++e) ok = mbar_wait(bar_v_empty(e % C::kRingV), phase_of(e, C::kRingV), abort_flag, p.status);
+        if (ok) ok = mbar_wait(bar_q_empty, static_cast<uint32_t>(seg & 1), abort_flag, p.status);
+        if (ok && on > 0) ok = mbar_wait(bar_o_done(i), static_cast<uint32_t>((on - 1) & 1), abort_flag, p.status);
     } else {
-        // ================= softmax: one thread per query row =================
+        // ================= softmax: one thread per query row and walker =================
+        const int i = warp >> 2, q4 = warp & 3;                       // walker, TMEM lane quadrant
         const int rep = p.rep, lr = 31 - __clz(rep);
-        const int r = warp * 32 + lane;
-        const int t = rt * (kRows >> lr) + (r >> lr);                 // node
-        const uint32_t lane_sel = static_cast<uint32_t>(warp * 32) << 16;
-        const uint32_t t_s = tmem_base + lane_sel, t_o = tmem_base + lane_sel + kOCol;
+        const int r = q4 * 32 + lane;
+        const int t = rt * (kTileRows >> lr) + (r >> lr);             // node
+        const uint32_t lane_sel = static_cast<uint32_t>(q4 * 32) << 16;
+        const uint32_t t_s = tmem_base + lane_sel + static_cast<uint32_t>(i * 128), t_o = tmem_base + lane_sel + kOCol + static_cast<uint32_t>(i * 128);
         const float scale = p.scale_log2;
-        int g0 = 0, fv0 = 0, on = 0;                                  // steps, steps whose V was fetched, accumulators of the segments before
+        float2 *ml = reinterpret_cast<float2 *>(smem + C::kMlOff);    // [walker][row]
+        int f0 = 0, g0 = 0, on = 0;                                   // as for the issuers
         pdl_wait();
-        read_lengths();
-        for (int si = seg_beg; ok;) {
-            if (n_steps == 0 && si == seg_beg) fv0 = early_v;
-            if (rt * kRows + warp * 32 < n * rep) {
-                const int n_act = (min(kRows, n * rep - rt * kRows) + 31) >> 5;      // softmax warps with rows
-                const uint32_t arrivals = warp == 0 ? static_cast<uint32_t>(C::kSoftmaxWarps + 1 - n_act) : 1u;
+        for (int seg = 0;; ++seg) {
+            ok = mbar_wait(bar_q_full, static_cast<uint32_t>(seg & 1), abort_flag, p.status);
+            if (!ok) break;
+            const Info it = infos[seg & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_q_empty);
+            const int n = it.n, mine = (it.n_steps + 1 - i) >> 1;
+            // A warp without rows passes a segment by.  (It cannot fall behind: the next segment but one waits for its look at this one.)
+            if (rows_before + q4 * 32 < n * rep && it.n_steps > 0) {
+                const int n_act = (min(kTileRows, n * rep - rows_before) + 31) >> 5;      // of the walker's warps with rows
                 const bool row_valid = t < n;
                 // nodes that this one sees; without masks the nodes are a chain
                 unsigned long long tree = 0;
@@ -358,20 +414,22 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                     tree = p.mask ? __ldcg(p.mask + static_cast<long long>(it.b) * p.n_max + t) : (2ull << t) - 1ull;
                     if (n < 64) tree &= (1ull << n) - 1ull;
                 }
-                // Keys of 32 pages, one page per lane, fetched eight steps ahead: how many of the page's rows count, or 256 | first node of a page of nodes.
-                auto load_meta = [&](int i) -> int {
-                    if (i < it.count) return __ldcg(p.stream_meta + it.first + i) & 0xff;
-                    const int g = i - it.count + t_first;
-                    if (i >= it.count + t_count) return 0;
-                    return g < tail_pages ? min(kPageTokens, len - g * kPageTokens) : 256 | (g - tail_pages) * kPageTokens;
+                // Keys of 32 pages (of eight steps of either walker), one page per lane, fetched that far ahead: how many of the page's rows count, or 256 |
+                // first node of a page of nodes.
+                auto load_meta = [&](int jj) -> int {
+                    const int x = (2 * (jj + lane / kStepPages) + i) * kStepPages + lane % kStepPages;
+                    if (x < it.count) return __ldcg(p.stream_meta + it.first + x) & 0xff;
+                    const int y = x - it.count + it.t_first;
+                    if (x >= it.count + it.t_count) return 0;
+                    return y < it.tail_pages ? min(kPageTokens, it.len - y * kPageTokens) : 256 | (y - it.tail_pages) * kPageTokens;
                 };
-                int meta = 0, meta_next = load_meta(lane);
-                float m = kNegInf, l = 0.f;                                   // reference (log2 units), row sum
-                for (int jj = 0; jj < n_steps; ++jj) {
+                int meta = 0, meta_next = load_meta(0);
+                float m = kNegInf, l = 0.f;                           // reference (log2 units), row sum
+                for (int jj = 0; jj < mine; ++jj) {
                     const int g = g0 + jj, b = g & 1;
                     if (jj % kBatch == 0) {
                         meta = meta_next;
-                        meta_next = load_meta((jj + kBatch) * kStepPages + lane);
+                        meta_next = load_meta(jj + kBatch);
                     }
                     int pg[kStepPages];
                     bool whole = true;
@@ -381,7 +439,7 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                         whole = whole && pg[e] == kPageTokens;
                     }
                     const uint32_t t_sb = t_s + static_cast<uint32_t>(b * kStepKeys);
-                    ok = mbar_wait(bar_s_full(b), static_cast<uint32_t>((g >> 1) & 1), abort_flag, p.status);
+                    ok = mbar_wait(bar_s_full(i, b), static_cast<uint32_t>((g >> 1) & 1), abort_flag, p.status);
                     if (!ok) break;
                     tc_fence_after();
 
@@ -431,7 +489,7 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                         l *= alpha;
                         m = m_new;
                         if (jj > 0) {
-                            ok = mbar_wait(bar_pv_done, static_cast<uint32_t>((g - on - 1) & 1), abort_flag, p.status);
+                            ok = mbar_wait(bar_pv_done(i), static_cast<uint32_t>((g - on - 1) & 1), abort_flag, p.status);
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll 1
@@ -466,20 +524,20 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                     }
                     // V rows that no row of the tile sees are cleared: 0 times whatever lies there must stay 0.  Those of the tail's last page and
                     // behind the last node (pool pages are zero behind a group's end).
-                    if (!whole && warp == 0) {
-                        const int fv = fv0 + g, x = fv % C::kRingV;
+                    if (!whole && q4 == 0) {
+                        const int f = f0 + 2 * jj + i, x = f % C::kRingV;
                         bool waited = false;
 #pragma unroll
                         for (int e = 0; e < kStepPages; ++e) {
                             const int rows = pg[e] & 256 ? min(kPageTokens, n - (pg[e] & 63)) : pg[e];
-                            if (jj * kStepPages + e < it.count || rows == 0 || rows == kPageTokens) continue;
-                            if (!waited) ok = mbar_wait(bar_v_full(x), phase_of(fv, C::kRingV), abort_flag, p.status);
+                            if ((2 * jj + i) * kStepPages + e < it.count || rows == 0 || rows == kPageTokens) continue;
+                            if (!waited) ok = mbar_wait(bar_v_full(x), phase_of(f, C::kRingV), abort_flag, p.status);
                             waited = true;
                             if (!ok) break;
                             uint8_t *page = smem + C::kVOff + x * C::kStepBytes + e * 2 * C::kGroupBytes;
-                            for (int i = lane; i < (kPageTokens - rows) * C::kBlocks * 8; i += 32) {    // 16-byte pieces
-                                const int row = rows + i / (C::kBlocks * 8), blk = i / 8 % C::kBlocks;
-                                *reinterpret_cast<uint4 *>(page + (row >> 3) * C::kGroupBytes + blk * 1024 + (row & 7) * 128 + i % 8 * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            for (int c = lane; c < (kPageTokens - rows) * C::kBlocks * 8; c += 32) {    // 16-byte pieces
+                                const int row = rows + c / (C::kBlocks * 8), blk = c / 8 % C::kBlocks;
+                                *reinterpret_cast<uint4 *>(page + (row >> 3) * C::kGroupBytes + blk * 1024 + (row & 7) * 128 + c % 8 * 16) = make_uint4(0u, 0u, 0u, 0u);
                             }
                         }
                         if (!ok) break;
@@ -488,63 +546,74 @@ __global__ void __launch_bounds__((kRows / 32 + 3) * 32, 2) tree_kernel(const __
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_n(bar_p_full(b), arrivals);
+                    if (lane == 0) mbar_arrive_n(bar_p_full(i, b), q4 == 0 ? static_cast<uint32_t>(5 - n_act) : 1u);
                     float lo0, hi0, lo1, hi1;
                     unpack2(ps2[0], lo0, hi0);
                     unpack2(ps2[1], lo1, hi1);
                     l += (lo0 + hi0) + (lo1 + hi1);
                 }
-                if (n_steps == 0) {                                           // a part without a step: the rows have seen nothing of it
-                    if (it.slot >= 0) p.part_lse[(static_cast<long long>(it.slot) * p.row_tiles + rt) * kTileRows + r] = kNegInf;
-                } else if (ok && (ok = mbar_wait(bar_o_done, static_cast<uint32_t>(on & 1), abort_flag, p.status))) {
-                    tc_fence_after();
-                    const float inv = l > 0.f ? 1.f / l : 0.f;
-                    const bool split = it.slot >= 0;
-                    const long long slot = static_cast<long long>(it.slot) * p.row_tiles + rt;
-                    if (split) p.part_lse[slot * kTileRows + r] = l > 0.f ? m + lg2(l) : kNegInf;
-                    // partial outputs [slot][D / 4][row][4]: a warp's store is one contiguous piece
-                    float4 *part = reinterpret_cast<float4 *>(p.part_o) + slot * (D / 4) * kTileRows + r;
-                    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
-                                 ((static_cast<long long>(it.b) * p.n_max + t) * p.Hq + it.kvh * rep + (r & (rep - 1))) * D);
+                if (ok && mine > 0) ok = mbar_wait(bar_o_done(i), static_cast<uint32_t>(on & 1), abort_flag, p.status);
+                // Both walkers' results of a row: references and sums go through shared memory, the accumulators lie in lanes that both warps
+                // read; each writes half of the channels.
+                if (mine == 0) { m = kNegInf; l = 0.f; }
+                ml[i * kTileRows + r] = make_float2(m, l);
+                tc_fence_before();
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                tc_fence_after();
+                const float2 other = ml[(1 - i) * kTileRows + r];
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");       // (the next segment's go to the same place)
+                const float top = fmaxf(m, other.x), mine_f = l > 0.f ? ex2(m - top) : 0.f, other_f = other.y > 0.f ? ex2(other.x - top) : 0.f;
+                const float sum = l * mine_f + other.y * other_f, inv = sum > 0.f ? 1.f / sum : 0.f;
+                const float f_mine = mine_f * inv, f_other = other_f * inv;
+                const bool split = it.slot >= 0;
+                const long long slot = static_cast<long long>(it.slot) * p.row_tiles + rt;
+                if (split && i == 0) p.part_lse[slot * kTileRows + r] = sum > 0.f ? top + lg2(sum) : kNegInf;
+                // partial outputs [slot][D / 4][row][4]: a warp's store is one contiguous piece
+                float4 *part = reinterpret_cast<float4 *>(p.part_o) + slot * (D / 4) * kTileRows + r;
+                uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
+                             ((static_cast<long long>(it.b) * p.n_max + t) * p.Hq + it.kvh * rep + (r & (rep - 1))) * D);
+                const uint32_t t_other = tmem_base + lane_sel + kOCol + static_cast<uint32_t>((1 - i) * 128);
 #pragma unroll 1
-                    for (int k = 0; k < D / 32; ++k) {
-                        uint32_t o[32];
-                        tmem_ld32_wait(t_o + static_cast<uint32_t>(k * 32), o);
-                        float f[32];
+                for (int k = i * (D / 32); k < (i + 1) * (D / 32) && ok; ++k) {      // 16 channels at a time
+                    uint32_t a[16], c[16];
+                    tmem_ld16_issue(t_o + static_cast<uint32_t>(k * 16), a);
+                    tmem_ld16_issue(t_other + static_cast<uint32_t>(k * 16), c);
+                    tmem_ld_wait();
+                    tmem_ld16_arrived(a);
+                    tmem_ld16_arrived(c);
+                    float f[16];
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) f[x] = l > 0.f ? __uint_as_float(o[x]) * inv : 0.f;      // a row that sees nothing: 0
-                        if (split) {
+                    for (int x = 0; x < 16; ++x)                      // (a walker that has seen nothing left nothing to read: 0, as for a row that sees no key)
+                        f[x] = (f_mine > 0.f ? __uint_as_float(a[x]) * f_mine : 0.f) + (f_other > 0.f ? __uint_as_float(c[x]) * f_other : 0.f);
+                    if (split) {
 #pragma unroll
-                            for (int x = 0; x < 8; ++x) part[(k * 8 + x) * kTileRows] = make_float4(f[4 * x], f[4 * x + 1], f[4 * x + 2], f[4 * x + 3]);
-                        } else if (row_valid) {
+                        for (int x = 0; x < 4; ++x) part[(k * 4 + x) * kTileRows] = make_float4(f[4 * x], f[4 * x + 1], f[4 * x + 2], f[4 * x + 3]);
+                    } else if (row_valid) {
 #pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                dst[k * 4 + x] = make_uint4(pack_bf16(f[8 * x], f[8 * x + 1]), pack_bf16(f[8 * x + 2], f[8 * x + 3]),
-                                                            pack_bf16(f[8 * x + 4], f[8 * x + 5]), pack_bf16(f[8 * x + 6], f[8 * x + 7]));
-                        }
+                        for (int x = 0; x < 2; ++x)
+                            dst[k * 2 + x] = make_uint4(pack_bf16(f[8 * x], f[8 * x + 1]), pack_bf16(f[8 * x + 2], f[8 * x + 3]),
+                                                        pack_bf16(f[8 * x + 4], f[8 * x + 5]), pack_bf16(f[8 * x + 6], f[8 * x + 7]));
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar_o_free);
                 }
-            } else if (n_steps > 0) {
-                // A warp without rows in this segment may have some in the next.  It keeps step with the others: ahead of them it would take phases
-                // before for those that it waits for, and arrive where the first warp has arrived for it; two segments behind it would wait for good.
-                ok = mbar_wait(bar_o_done, static_cast<uint32_t>(on & 1), abort_flag, p.status);
-                if (ok && lane == 0) mbar_arrive(bar_o_free);
+                tc_fence_before();
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive_n(bar_o_free, warp == 0 ? static_cast<uint32_t>(9 - 2 * n_act) : 1u);      // (also for those without rows)
+            } else if (it.n_steps == 0 && i == 0 && it.slot >= 0 && rows_before + q4 * 32 < n * rep) {
+                // a part without a step: its rows have seen nothing of it
+                p.part_lse[(static_cast<long long>(it.slot) * p.row_tiles + rt) * kTileRows + r] = kNegInf;
             }
-            if (n_steps > 0) ++on;
-            g0 += n_steps;
-            if (++si >= seg_end) break;
-            it = segment(si);
-            read_lengths();
+            if (!ok) break;
+            on += mine > 0 ? 1 : 0;
+            g0 += mine;
+            f0 += it.n_steps + (it.n_steps == 0 && seg == 0 ? early_of(it.count) : 0);
+            if (!it.more) break;
         }
     }
 
     // ---- teardown ----
     tc_fence_before();
     __syncthreads();
-    if (warp == C::kMmaWarp) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
     }
@@ -623,30 +692,20 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 8) tree_merge_kernel(const _
 
 }  // namespace
 
-template <int D, int kRows>
-static cudaError_t prepare()
-{
-    return cudaFuncSetAttribute(tree_kernel<D, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D, kRows>::kSmemBytes);
-}
 cudaError_t prepare_tree(int head_dim)
 {
-    if (head_dim != 128 && head_dim != 64) return cudaErrorInvalidValue;
-    const cudaError_t e = head_dim == 128 ? prepare<128, 64>() : prepare<64, 64>();
-    return e != cudaSuccess ? e : head_dim == 128 ? prepare<128, 128>() : prepare<64, 128>();
+    if (head_dim == 128) return cudaFuncSetAttribute(tree_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmemBytes);
+    if (head_dim == 64) return cudaFuncSetAttribute(tree_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes);
+    return cudaErrorInvalidValue;
 }
 
-template <int D, int kRows>
-static cudaError_t launch(const TreeParams &p, int grid, cudaStream_t st)
-{
-    return launch_pdl(tree_kernel<D, kRows>, dim3(grid), dim3(Cfg<D, kRows>::kThreads), Cfg<D, kRows>::kSmemBytes, st, p);
-}
 cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_t st)
 {
-    if (head_dim != 128 && head_dim != 64) return cudaErrorInvalidValue;
-    const bool few = p.n_max * p.rep <= 64;
-    if (few ? p.row_tiles != 1 || p.box_tokens * p.rep > 64 : p.box_tokens * p.rep > 128) return cudaErrorInvalidValue;
-    const cudaError_t e = head_dim == 128 ? (few ? launch<128, 64>(p, grid, st) : launch<128, 128>(p, grid, st))
-                                          : (few ? launch<64, 64>(p, grid, st) : launch<64, 128>(p, grid, st));
+    cudaError_t e;
+    if (p.box_tokens * p.rep > kTileRows) return cudaErrorInvalidValue;
+    if (head_dim == 128) e = launch_pdl(tree_kernel<128>, dim3(grid), dim3(kThreads), Cfg<128>::kSmemBytes, st, p);
+    else if (head_dim == 64) e = launch_pdl(tree_kernel<64>, dim3(grid), dim3(kThreads), Cfg<64>::kSmemBytes, st, p);
+    else return cudaErrorInvalidValue;
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 

@@ -165,7 +165,7 @@ def test_runs_of_parts_across_requests(model, batch, n_max):
     try:
         c.call()
         tiles = -(-n_max * (model[0] // model[1]) // 128)
-        assert enl.enl_plan_inspect(c.cache)["n_items"] == 296 // tiles * tiles, "equal parts: not what this test is for"
+        assert enl.enl_plan_inspect(c.cache)["n_items"] == 148 // tiles * tiles, "equal parts: not what this test is for"
         c.check()
         first = c.out.clone()
         for _ in range(3):

@@ -211,14 +211,14 @@ def test_plan_larger_than_its_buffers(host):
 
 
 def test_grid_and_splits(host):
-    """Splits until two CTAs per multiprocessor have work, as few as come to the same number of steps, and none where scratch buffer or stream
+    """Splits until every multiprocessor has a CTA, as few as come to the same number of steps, and none where scratch buffer or stream
     are too short for them."""
     c = Host(host)
     # 9 cached pages, a table of 32, one page of nodes: 42; a step of four pages each
     assert c.call() == enl.ENL_OK
     assert (host.fake_grid(), host.fake_splits(), host.fake_box()) == (8 * 11, 11, 16) and host.fake_deep() == 1
     # 64 nodes are two tiles of rows, and four pages themselves
-    assert c.call(n_max=64) == enl.ENL_OK and (host.fake_grid(), host.fake_splits(), host.fake_box()) == (8 * 2 * 12, 12, 32)
+    assert c.call(n_max=64) == enl.ENL_OK and (host.fake_grid(), host.fake_splits(), host.fake_box()) == (8 * 2 * 6, 6, 32)
     c.kinds()
     assert c.call(sel=(), max_blocks=1, n_max=1) == enl.ENL_OK and (host.fake_grid(), host.fake_splits()) == (8, 1) and c.kinds() == "t"        # an empty plan
     c = Host(host, scratch_bytes=100000)
@@ -229,7 +229,7 @@ def test_grid_and_splits(host):
     # two requests: the longer one is cut into more
     c = Host(host)
     assert c.call(sel=(0, 1, 2, 3), batch=2, cu_sel=np.array([0, 0, 4], np.int32)) == enl.ENL_OK
-    assert host.fake_grid() <= 296 and host.fake_grid() % 8 == 0 and host.fake_splits() > 4
+    assert host.fake_grid() <= 148 and host.fake_grid() % 8 == 0 and host.fake_splits() > 4
 
 
 @pytest.mark.parametrize("batch,lens,blocks,n_max,kv", [(16, (180, 230), 52, 24, 8), (16, (180, 230), 52, 64, 8), (3, (1100, 1500), 40, 16, 8), (40, (70, 140), 30, 8, 8),
@@ -271,10 +271,10 @@ def test_shares_of_several_requests(host, batch, lens, blocks, n_max, kv):
         if host.fake_splits() > 1:
             assert host.fake_unit(r * kv + h, 1) == len(parts) and (len(parts) == 1 or host.fake_unit(r * kv + h, 0) == parts[0][3])
     work = [sum((b - a) / whole * (pages[head >> 16] + blocks + -(-n_max // 16)) for head, _, _, _, a, b, whole in seg[i:j]) for i, j in zip(off, off[1:])]
-    units_per_place = batch * kv * tiles / 296
+    units_per_place = batch * kv * tiles / 148
     if units_per_place < 1:
-        assert groups * tiles <= 296
-        assert max(work) <= sum(work) / (296 // tiles) * 1.35 + 4 * 4, (max(work), sum(work) / (296 // tiles))
+        assert groups * tiles <= 148
+        assert max(work) <= sum(work) / (148 // tiles) * 1.35 + 4 * 4, (max(work), sum(work) / (148 // tiles))
 
 
 # ---- the calls without a cache: nothing is followed before everything has been looked at ---------------------------------------
