@@ -11,7 +11,8 @@ using namespace enl;
 namespace {
 
 constexpr int kStepPages = kStepKeys / kPageTokens;
-constexpr int kMergeSteps = 4;      // what putting parts together costs, in steps of a CTA
+constexpr int kMergeSteps = 6;      // what putting parts together costs, in steps of a CTA
+constexpr double kAlone = 0.67;     // how long a step takes where the memory is not what is waited for
 constexpr int kEarly = 8, kEarlyMerge = 2;      // steps fetched before the wait for the previous kernel; where that is a merge kernel, whose loads they hold up
 constexpr int kSegmentSteps = 2;    // what another segment of a CTA costs
 
@@ -165,20 +166,21 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         sh.heads = d.n_kv_heads;
         int64_t n_groups = d.n_kv_heads * parts[0];
         if (B > 1) {
-            // Equal parts leave places empty, or the longest streams with the longest parts (16 requests of 3200 cached keys and
-            // tails of 256 to 768, 8 kv heads: ... us); runs are as long for every CTA, but cost most CTAs a second segment.
-            int64_t total = 0, longest = 0, cut = 0;
+            // Equal parts, or runs that are as long for every CTA but cost most CTAs a second segment and most units a merge.  What either takes, in steps
+            // of a CTA while all run (0.75 us: the memory's pace; alone a CTA takes 0.5): a wave of few CTAs is as fast as its longest one.
+            int64_t total = 0, ctas = 0, longest = 0;
+            bool cut = false;
             std::vector<int64_t> steps(B);
             for (int b = 0; b < B; ++b) {
                 steps[b] = steps_of(pages[b]);
                 total += steps[b] * d.n_kv_heads;
+                ctas += parts[b] * d.n_kv_heads;
                 longest = std::max(longest, steps_of((pages[b] + parts[b] - 1) / parts[b]));
                 cut |= parts[b] > 1;
             }
-            const int64_t waves = (n_units + places - 1) / places;
-            const int64_t by_parts = n_units > places ? std::max(longest, (total + places - 1) / places + (waves - 1) * kSegmentSteps + longest / 2)
-                                                      : longest + (cut ? kMergeSteps : 0);
-            const int64_t by_runs = (total + places - 1) / places + kSegmentSteps + kMergeSteps;
+            const double mean = static_cast<double>(total) / ctas, rest = static_cast<double>(ctas % places) / places;
+            const double by_parts = mean * (ctas / places + (rest > 0.0 ? std::max(kAlone, rest) : 0.0)) + (longest - mean) * kAlone + (cut ? kMergeSteps : 0);
+            const double by_runs = static_cast<double>(total) / places + kSegmentSteps + kMergeSteps;
             sh.units.assign(n_units, make_int2(0, 0));
             if (by_runs < by_parts && 2 * places <= slots) sh.runs(steps, places);
             else sh.equal(parts);

@@ -112,6 +112,43 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
     const int group = p.row_tiles == 1 ? static_cast<int>(blockIdx.x) : static_cast<int>(blockIdx.x) / p.row_tiles;
     const int rt = p.row_tiles == 1 ? 0 : static_cast<int>(blockIdx.x) - group * p.row_tiles;
     const int rows_before = rt * kTileRows;
+    struct Part { int b, kvh, slot, first, count, from, to, whole; };
+    auto segment = [&](int i) -> Part {
+        Part w;
+        if (p.batch == 1) {
+            w.b = 0;
+            w.kvh = group / p.n_splits;
+            w.from = group - w.kvh * p.n_splits;
+            w.to = w.from + 1;
+            w.whole = p.n_splits;
+            w.slot = p.n_splits > 1 ? group : -1;
+            w.first = static_cast<int>(static_cast<long long>(p.n_entries) * w.from / p.n_splits);
+            w.count = static_cast<int>(static_cast<long long>(p.n_entries) * w.to / p.n_splits) - w.first;
+        } else {
+            const int4 *src = reinterpret_cast<const int4 *>(p.segments + i);
+            const int4 x = __ldcg(src), y = __ldcg(src + 1);
+            w.b = x.x >> 16; w.kvh = x.x & 0xffff; w.slot = x.y; w.first = x.z; w.count = x.w;
+            w.from = y.x; w.to = y.y; w.whole = y.z;
+        }
+        return w;
+    };
+    int seg_beg = 0, seg_end = 1;
+    // (for the producers only: under the set-up, a round trip each)
+    Part it = {0, 0, 0, 0, 0, 0, 0, 1};
+    uint32_t next = kZeroPage;                // where the pages of the first eight steps lie (see below), of the cached ones so far
+    if (warp == kKWarp || warp == kVWarp) {
+        if (p.batch > 1) {
+            seg_beg = __ldcg(p.segment_off + group);
+            seg_end = __ldcg(p.segment_off + group + 1);
+        }
+        it = segment(seg_beg);
+        if (lane < it.count) next = static_cast<uint32_t>(__ldcg(p.stream_page + it.first + lane));
+        if (lane < 4) {
+            const CUtensorMap *tm = warp == kKWarp ? (lane == 0 ? &p.tm_kpool : lane == 1 ? &p.tm_q : lane == 2 ? &p.tm_ktail : &p.tm_knew)
+                                                   : (lane == 0 ? &p.tm_vpool : lane == 1 ? &p.tm_vtail : &p.tm_vnew);
+            asm volatile("prefetch.tensormap [%0];" ::"l"(tm) : "memory");
+        }
+    }
 
     // ---- set-up ----
     if (warp == kMmaWarp) {
@@ -154,34 +191,9 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
         const uint32_t ring = sbase + static_cast<uint32_t>(is_k ? C::kKOff : C::kVOff), full0 = is_k ? bar_k_full(0) : bar_v_full(0),
                        empty0 = is_k ? bar_k_empty(0) : bar_v_empty(0);
         const int places = is_k ? C::kRingK : C::kRingV;
-        struct Part { int b, kvh, slot, first, count, from, to, whole; };
-        auto segment = [&](int i) -> Part {
-            Part w;
-            if (p.batch == 1) {
-                w.b = 0;
-                w.kvh = group / p.n_splits;
-                w.from = group - w.kvh * p.n_splits;
-                w.to = w.from + 1;
-                w.whole = p.n_splits;
-                w.slot = p.n_splits > 1 ? group : -1;
-                w.first = static_cast<int>(static_cast<long long>(p.n_entries) * w.from / p.n_splits);
-                w.count = static_cast<int>(static_cast<long long>(p.n_entries) * w.to / p.n_splits) - w.first;
-            } else {
-                const int4 *src = reinterpret_cast<const int4 *>(p.segments + i);
-                const int4 x = __ldcg(src), y = __ldcg(src + 1);
-                w.b = x.x >> 16; w.kvh = x.x & 0xffff; w.slot = x.y; w.first = x.z; w.count = x.w;
-                w.from = y.x; w.to = y.y; w.whole = y.z;
-            }
-            return w;
-        };
-        int seg_beg = 0, seg_end = 1;
-        if (p.batch > 1) {
-            seg_beg = __ldcg(p.segment_off + group);
-            seg_end = __ldcg(p.segment_off + group + 1);
-        }
         // Lengths: a request that has ended, or has no nodes, leaves nothing to do; a tail is as long as its block table at most.  What comes from
         // the kernel before is read past the L1, since this one may have started while that one ran.
-        Part it = segment(seg_beg), ahead = it;                      // this segment, and the next one, fetched a segment ahead
+        Part ahead = it;                                             // the next segment, fetched a segment ahead
         int2 raw = make_int2(0, 0), raw_ahead = raw;                                         // rows of the tail and nodes, as they are in memory
         auto lengths = [&](int b) { return make_int2(__ldcg(p.tail_len + b), p.n_new ? __ldcg(p.n_new + b) : p.n_max); };
         int len = 0, n = 0, t_first = 0, t_count = 0, tail_pages = 0, n_steps = 0;
@@ -243,7 +255,7 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
         // out to have no rows leaves them, and its Q tile, to be passed over.)
         static_assert(C::kRingK <= kBatch && C::kRingV <= kBatch, "the early steps' pages are of one batch");
         const int early = early_of(it.count);
-        uint32_t cur = 0, next = where(lane);                        // (of the cached pages so far)
+        uint32_t cur = 0;
         int f = 0;                                                   // steps fetched
         for (; f < early; ++f) fetch(__shfl_sync(kFull, next, f * kStepPages + lane % kStepPages), f);
         pdl_wait();
@@ -619,18 +631,19 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
     }
 }
 
-// Puts the parts of a unit together: out = sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  A warp takes four channels of 32 / kLanes rows; kLanes
-// lanes share a row and take every kLanes-th part, up to kAhead at a time, all of whose loads are on their way at once.  No shared memory and few
+// Puts the parts of a unit together: out = sum_s 2^(lse_s - M) o_s / sum_s 2^(lse_s - M).  A warp takes eight channels of 32 / kLanes rows; kLanes
+// lanes share a row and take every kLanes-th part, four at a time, all of whose loads are on their way at once.  No shared memory and few
 // registers, so that its CTAs find a place beside those of the attention kernel and wait there for its end; nor does a load wait for
 // another (a row that turns out to be none has read what lay in the scratch buffer).  grid.x: units and groups of rows, grid.y: channels.
 constexpr int kMergeWarps = 4;
-template <int D, int kLanes, int kAhead>
+constexpr int kMergeAhead = 4;
+template <int D, int kLanes>
 __global__ void __launch_bounds__(kMergeWarps * 32, 8) tree_merge_kernel(const __grid_constant__ TreeMergeParams p)
 {
     constexpr int kWarpRows = 32 / kLanes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, of = lane / kWarpRows;
     const int lr = 31 - __clz(p.rep);
-    const int unit = static_cast<int>(blockIdx.x) / p.row_groups, quad = static_cast<int>(blockIdx.y);
+    const int unit = static_cast<int>(blockIdx.x) / p.row_groups, quad = 2 * static_cast<int>(blockIdx.y);
     const int row = ((static_cast<int>(blockIdx.x) - unit * p.row_groups) * kMergeWarps + warp) * kWarpRows + lane % kWarpRows;
     const int b = unit / p.Hkv, kvh = unit - b * p.Hkv, tile = row / kTileRows, r = row % kTileRows;
     // (the plan is not new any more: the kernel before has waited for it before it let this one start)
@@ -640,54 +653,60 @@ __global__ void __launch_bounds__(kMergeWarps * 32, 8) tree_merge_kernel(const _
     if (head.y < 2 || tile >= p.row_tiles) return;          // (the same for the whole warp: it has rows of one tile)
     const int len = __ldcg(p.tail_len + b), n_new = p.n_new ? __ldcg(p.n_new + b) : p.n_max;
     const long long slot0 = static_cast<long long>(head.x) * p.row_tiles + tile;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float acc[8] = {};
     float m = kNegInf, l = 0.f;
-    for (int s0 = of; s0 < head.y; s0 += kAhead * kLanes) {
-        float lse[kAhead];
-        float4 x[kAhead];
+    for (int s0 = of; s0 < head.y; s0 += kMergeAhead * kLanes) {
+        float lse[kMergeAhead];
+        float4 x[kMergeAhead][2];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kMergeAhead; ++u) {
             const int s = s0 + u * kLanes;
             lse[u] = kNegInf;
             if (s < head.y) {
                 const long long slot = slot0 + static_cast<long long>(s) * p.row_tiles;
+                const float4 *o = reinterpret_cast<const float4 *>(p.part_o) + (slot * (D / 4) + quad) * kTileRows + r;
                 lse[u] = __ldcg(p.part_lse + slot * kTileRows + r);
-                x[u] = __ldcg(reinterpret_cast<const float4 *>(p.part_o) + (slot * (D / 4) + quad) * kTileRows + r);
+                x[u][0] = __ldcg(o);
+                x[u][1] = __ldcg(o + kTileRows);
             }
         }
         float m_new = m;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) m_new = fmaxf(m_new, lse[u]);
+        for (int u = 0; u < kMergeAhead; ++u) m_new = fmaxf(m_new, lse[u]);
         if (m_new == kNegInf) continue;                     // parts that saw no key
         const float alpha = ex2(m - m_new);
         l *= alpha;
-        acc.x *= alpha; acc.y *= alpha; acc.z *= alpha; acc.w *= alpha;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[c] *= alpha;
         m = m_new;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
+        for (int u = 0; u < kMergeAhead; ++u) {
             if (lse[u] == kNegInf) continue;
             const float f = ex2(lse[u] - m);
             l += f;
-            acc.x = fmaf(f, x[u].x, acc.x); acc.y = fmaf(f, x[u].y, acc.y);
-            acc.z = fmaf(f, x[u].z, acc.z); acc.w = fmaf(f, x[u].w, acc.w);
+            acc[0] = fmaf(f, x[u][0].x, acc[0]); acc[1] = fmaf(f, x[u][0].y, acc[1]);
+            acc[2] = fmaf(f, x[u][0].z, acc[2]); acc[3] = fmaf(f, x[u][0].w, acc[3]);
+            acc[4] = fmaf(f, x[u][1].x, acc[4]); acc[5] = fmaf(f, x[u][1].y, acc[5]);
+            acc[6] = fmaf(f, x[u][1].z, acc[6]); acc[7] = fmaf(f, x[u][1].w, acc[7]);
         }
     }
     // the lanes of a row, in a fixed order
 #pragma unroll
     for (int o = kWarpRows; o < 32; o <<= 1) {
-        const float m2 = __shfl_xor_sync(kFull, m, o), l2 = __shfl_xor_sync(kFull, l, o);
-        const float4 x = make_float4(__shfl_xor_sync(kFull, acc.x, o), __shfl_xor_sync(kFull, acc.y, o), __shfl_xor_sync(kFull, acc.z, o), __shfl_xor_sync(kFull, acc.w, o));
-        const float top = fmaxf(m, m2), a = m == kNegInf ? 0.f : ex2(m - top), c = m2 == kNegInf ? 0.f : ex2(m2 - top);
-        l = l * a + l2 * c;
-        acc.x = acc.x * a + x.x * c; acc.y = acc.y * a + x.y * c; acc.z = acc.z * a + x.z * c; acc.w = acc.w * a + x.w * c;
+        const float m2 = __shfl_xor_sync(kFull, m, o), top = fmaxf(m, m2);
+        const float a = m == kNegInf ? 0.f : ex2(m - top), c = m2 == kNegInf ? 0.f : ex2(m2 - top);
+        l = l * a + __shfl_xor_sync(kFull, l, o) * c;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] = acc[k] * a + __shfl_xor_sync(kFull, acc[k], o) * c;
         m = top;
     }
     const int n = len < 0 ? 0 : min(n_new, p.n_max);
     if (of != 0 || row >= n << lr) return;
     const float inv = l > 0.f ? 1.f / l : 0.f;
-    uint2 *dst = reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(p.out) +
+    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
                  ((static_cast<long long>(b) * p.n_max + (row >> lr)) * p.Hq + kvh * p.rep + (row & (p.rep - 1))) * D + quad * 4);
-    *dst = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    *dst = make_uint4(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv), pack_bf16(acc[4] * inv, acc[5] * inv),
+                      pack_bf16(acc[6] * inv, acc[7] * inv));
 }
 
 }  // namespace
@@ -709,14 +728,19 @@ cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-template <int D>
-static cudaError_t launch_merge(TreeMergeParams p, int batch, int most, cudaStream_t st)
+template <int D, int kLanes>
+static cudaError_t launch_merge(TreeMergeParams p, int batch, cudaStream_t st)
 {
-    // Few parts (calls with many units): lanes side by side; many: eight lanes a row, five parts each at a time.
-    const int lanes = most > 4 ? 8 : 1, rows = kMergeWarps * 32 / lanes;
-    p.row_groups = (p.n_max * p.rep + rows - 1) / rows;
-    const dim3 grid(static_cast<unsigned>(batch) * p.Hkv * p.row_groups, D / 4), block(kMergeWarps * 32);
-    return lanes == 8 ? launch_pdl(tree_merge_kernel<D, 8, 5>, grid, block, 0, st, p) : launch_pdl(tree_merge_kernel<D, 1, 4>, grid, block, 0, st, p);
+    constexpr int kRows = kMergeWarps * 32 / kLanes;
+    p.row_groups = (p.n_max * p.rep + kRows - 1) / kRows;
+    return launch_pdl(tree_merge_kernel<D, kLanes>, dim3(static_cast<unsigned>(batch) * p.Hkv * p.row_groups, D / 8), dim3(kMergeWarps * 32), 0, st, p);
+}
+// as many lanes a row as it takes to have all parts on their way at once
+template <int D>
+static cudaError_t launch_merge(const TreeMergeParams &p, int batch, int most, cudaStream_t st)
+{
+    return most <= kMergeAhead ? launch_merge<D, 1>(p, batch, st) : most <= 2 * kMergeAhead ? launch_merge<D, 2>(p, batch, st)
+         : most <= 4 * kMergeAhead ? launch_merge<D, 4>(p, batch, st) : launch_merge<D, 8>(p, batch, st);
 }
 cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, int most, cudaStream_t st)
 {

@@ -154,7 +154,7 @@ def test_one_long_request_among_short_ones():
     run((8, 2, 128), [[700] * 9, [20], [33], [16, 16]], [900, 3, 0, 17], [20, 20, 1, 7], 20)
 
 
-@pytest.mark.parametrize("model,batch,n_max", [((8, 2, 64), 64, 5), ((16, 2, 128), 60, 12), ((32, 2, 128), 40, 24), ((8, 2, 128), 62, 30)], ids=str)
+@pytest.mark.parametrize("model,batch,n_max", [((8, 2, 64), 80, 5), ((16, 2, 128), 79, 12), ((32, 2, 128), 27, 24), ((8, 2, 128), 76, 30)], ids=str)
 def test_runs_of_parts_across_requests(model, batch, n_max):
     """Streams that do not divide into equal parts: most CTAs take the end of one and the beginning of the next, with other counts of rows; some
     of them belong to requests that have ended or have no nodes, the first ones too."""
