@@ -11,21 +11,37 @@ using namespace enl;
 namespace {
 
 constexpr int kStepPages = kStepKeys / kPageTokens;
-constexpr int kMergeSteps = 6;      // what putting parts together costs, in steps of a CTA
-constexpr double kAlone = 0.67;     // how long a step takes where the memory is not what is waited for
-constexpr int kEarly = 8, kEarlyMerge = 2;      // steps fetched before the wait for the previous kernel; where that is a merge kernel, whose loads they hold up
-constexpr int kSegmentSteps = 2;    // what another segment of a CTA costs
+// What calls take, in steps (of 64 keys) of a CTA while all CTAs run: 0.75 us, the memory's pace.
+constexpr double kMerge = 5.0;      // putting parts together
+constexpr double kSegment = 3.0;    // runs: another segment of a CTA
+constexpr double kPair = 1.7;      // a step of either walker where the memory is not what is waited for
+constexpr int kSegmentSteps = 2;    // runs do not begin or end closer to a unit's ends
+// Steps fetched before the wait for the previous kernel.  Where that is a merge kernel, whose loads they hold up, four if parts have kLongPart steps
+// and two if not (one token over 33 000 keys 29.9 us with two, 29.1 with four, 29.5 with six; 64 nodes over 7400 20.7, 21.2, 22.3).
+constexpr int kEarly = 8, kEarlyLong = 4, kEarlyShort = 2, kLongPart = 16;
 
 int64_t steps_of(int64_t pages) { return (pages + kStepPages - 1) / kStepPages; }
 
-// How many equal parts a stream of `pages` pages gets that may have `most`: the fewest that come to as few steps per CTA as `most` would, and
-// one where that does not save what putting them together costs.
-int64_t parts_for(int64_t pages, int64_t most)
+// Equal parts: those of the streams (`pages[b]` pages each, `heads` of them) that are longer than `piece` are cut.  `parts` receives how many parts,
+// the return value is what the call takes with one CTA a part and `places` of them at once (a negative one: too many for `slots` results).
+double equal_parts(const std::vector<int64_t> &pages, int heads, int64_t piece, int64_t places, int64_t slots, std::vector<int64_t> &parts)
 {
-    most = std::max<int64_t>(1, std::min(most, steps_of(pages)));
-    const int64_t steps = steps_of((pages + most - 1) / most);
-    if (steps_of(pages) <= steps + kMergeSteps) return 1;
-    return (pages + steps * kStepPages - 1) / (steps * kStepPages);
+    int64_t ctas = 0, total = 0, longest = 0, partial = 0;
+    for (size_t b = 0; b < pages.size(); ++b) {
+        parts[b] = (pages[b] + piece - 1) / piece;
+        ctas += parts[b] * heads;
+        partial += parts[b] > 1 ? parts[b] * heads : 0;
+        total += steps_of(pages[b]) * heads;
+        longest = std::max(longest, steps_of((pages[b] + parts[b] - 1) / parts[b]));
+    }
+    if (partial > slots || (partial > 0 && ctas > places)) return -1.0;
+    // whole waves at the memory's pace, then the CTAs of the last one, which may be too few for it
+    const double mean = static_cast<double>(total) / ctas, rest = static_cast<double>(ctas % places);
+    auto pairs = [](double steps) { return kPair * std::ceil(steps / 2.0); };
+    double cost = ctas / places * mean + (partial > 0 ? kMerge : 0.0);
+    if (ctas <= places) cost = std::max(static_cast<double>(total) / places, pairs(static_cast<double>(longest))) + (partial > 0 ? kMerge : 0.0);
+    else cost += (rest > 0.0 ? std::max(rest / places * mean, pairs(mean)) : 0.0) + 0.5 * (longest - mean);
+    return cost;
 }
 
 // What the CTAs of a call of several requests do, made for streams of `pages[b]` pages (each of them `heads` times) and `groups` places for CTAs:
@@ -145,42 +161,32 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         // that turns out short cost little, since all CTAs run at once, one on a multiprocessor.
         const int64_t slot_bytes = static_cast<int64_t>(kTileRows) * (d.head_dim + 1) * 4 * row_tiles;
         const int64_t places = std::max<int64_t>(1, c->n_sm / row_tiles), slots = d.scratch_bytes / slot_bytes;
-        std::vector<int64_t> pages(B), parts(B, 1);
+        std::vector<int64_t> pages(B), parts(B), tried(B);
         for (int b = 0; b < B; ++b) {
             pages[b] = ceil_div(a->n_max, kPageTokens) + static_cast<int64_t>(a->max_blocks);
             for (int s = cu_sel[b]; s < cu_sel[b + 1]; ++s) pages[b] += std::max(1, ceil_div(c->sel_len[s], kPageTokens));
         }
-        // equal parts: of as few pages as there are places for
-        const int64_t n_units = static_cast<int64_t>(B) * d.n_kv_heads, few = std::min(places, slots);
-        if (n_units < few) {
-            int64_t lo = 1, hi = *std::max_element(pages.begin(), pages.end());
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) / 2;
-                int64_t n = 0;
-                for (int b = 0; b < B; ++b) n += (pages[b] + mid - 1) / mid * d.n_kv_heads;
-                if (n <= few) hi = mid; else lo = mid + 1;
+        const int64_t n_units = static_cast<int64_t>(B) * d.n_kv_heads, longest = *std::max_element(pages.begin(), pages.end());
+        double by_parts = equal_parts(pages, d.n_kv_heads, longest, places, slots, parts);
+        for (int64_t k = 2; k * d.n_kv_heads <= places && k <= longest; ++k) {
+            const double cost = equal_parts(pages, d.n_kv_heads, (longest + k - 1) / k, places, slots, tried);
+            if (cost >= 0.0 && cost < by_parts - 1e-9) {              // (of equal costs the fewest parts)
+                by_parts = cost;
+                parts = tried;
             }
-            for (int b = 0; b < B; ++b) parts[b] = parts_for(pages[b], (pages[b] + hi - 1) / hi);
         }
         Shares sh;
         sh.heads = d.n_kv_heads;
         int64_t n_groups = d.n_kv_heads * parts[0];
         if (B > 1) {
-            // Equal parts, or runs that are as long for every CTA but cost most CTAs a second segment and most units a merge.  What either takes, in steps
-            // of a CTA while all run (0.75 us: the memory's pace; alone a CTA takes 0.5): a wave of few CTAs is as fast as its longest one.
-            int64_t total = 0, ctas = 0, longest = 0;
-            bool cut = false;
+            // Or runs, as long for every CTA, which cost most CTAs a second segment and most units a merge.
+            int64_t total = 0;
             std::vector<int64_t> steps(B);
             for (int b = 0; b < B; ++b) {
                 steps[b] = steps_of(pages[b]);
                 total += steps[b] * d.n_kv_heads;
-                ctas += parts[b] * d.n_kv_heads;
-                longest = std::max(longest, steps_of((pages[b] + parts[b] - 1) / parts[b]));
-                cut |= parts[b] > 1;
             }
-            const double mean = static_cast<double>(total) / ctas, rest = static_cast<double>(ctas % places) / places;
-            const double by_parts = mean * (ctas / places + (rest > 0.0 ? std::max(kAlone, rest) : 0.0)) + (longest - mean) * kAlone + (cut ? kMergeSteps : 0);
-            const double by_runs = static_cast<double>(total) / places + kSegmentSteps + kMergeSteps;
+            const double by_runs = static_cast<double>(total) / places + kSegment + kMerge;
             sh.units.assign(n_units, make_int2(0, 0));
             if (by_runs < by_parts && 2 * places <= slots) sh.runs(steps, places);
             else sh.equal(parts);
@@ -278,7 +284,7 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
     p.row_tiles = row_tiles;
     p.n_splits = c->plan_splits;
     p.n_entries = c->tree_entries;
-    p.early_steps = c->plan_splits > 1 ? kEarlyMerge : kEarly;
+    p.early_steps = c->plan_splits == 1 ? kEarly : c->tree_entries / c->plan_splits >= kLongPart * kStepPages ? kEarlyLong : kEarlyShort;
     p.scale_log2 = 1.4426950408889634f / sqrtf(static_cast<float>(d.head_dim));
 
     p.part_o = c->scratch;

@@ -49,20 +49,21 @@ struct Cfg {
     static constexpr int kTileBytes  = kBlocks * kBlockBytes;
     static constexpr int kGroupBytes = kBlocks * 1024;        // eight rows of K or V
     static constexpr int kStepBytes  = kStepKeys / 8 * kGroupBytes;
-    // Steps whose K, and whose V, are in shared memory at once (V stays until its step's softmax is done).  Even numbers: a place belongs to one
-    // walker, whose waits for it then follow one another.
-    static constexpr int kRingK      = D == 64 ? 8 : 4;
+    // Steps whose K, and whose V, are in shared memory at once: all there is room for.  K of a step is wanted two steps of its walker ahead: with
+    // four places its load had less time than it takes when the memory is busy (16 requests on 128 CTAs 51.7 us, now 47.2).  Even numbers: a
+    // place belongs to one walker, whose waits for it then follow one another.
+    static constexpr int kRingK      = D == 64 ? 8 : 6;
     static constexpr int kRingV      = D == 64 ? 8 : 6;
     static_assert(kRingK % 2 == 0 && kRingV % 2 == 0, "a place, a walker");
     static constexpr int kEarly      = kRingK < kRingV ? kRingK : kRingV;
     static constexpr int kKOff       = kTileBytes;
     static constexpr int kVOff       = kKOff + kRingK * kStepBytes;
-    static constexpr int kMlOff      = kVOff + kRingV * kStepBytes;      // [walker][row] reference and sum
-    static constexpr int kInfoOff    = kMlOff + 2 * kTileRows * 8;       // what the warps have to know of a segment, [2]
+    static constexpr int kMlOff      = kVOff + kRingV * kStepBytes;      // [row] what the walkers tell each other
+    static constexpr int kInfoOff    = kMlOff + kTileRows * 8;           // what the warps have to know of a segment, [2]
     static constexpr int kBarOff     = kInfoOff + 2 * 64;
     static constexpr int kBars       = 15 + 2 * (kRingK + kRingV);
     static constexpr int kSmemBytes  = kBarOff + 8 * kBars + 8;
-    static_assert(kSmemBytes <= 232448 - 2048, "a CTA of the merge kernel beside it");
+    static_assert(kSmemBytes <= 233472 - 2 * 1024, "a CTA of the merge kernel beside it (each takes 1 KB for itself)");
 };
 
 __device__ __forceinline__ int pages_of(int rows) { return (rows + kPageTokens - 1) / kPageTokens; }
@@ -406,7 +407,7 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
         const uint32_t lane_sel = static_cast<uint32_t>(q4 * 32) << 16;
         const uint32_t t_s = tmem_base + lane_sel + static_cast<uint32_t>(i * 128), t_o = tmem_base + lane_sel + kOCol + static_cast<uint32_t>(i * 128);
         const float scale = p.scale_log2;
-        float2 *ml = reinterpret_cast<float2 *>(smem + C::kMlOff);    // [walker][row]
+        float2 *ml = reinterpret_cast<float2 *>(smem + C::kMlOff);
         int f0 = 0, g0 = 0, on = 0;                                   // as for the issuers
         pdl_wait();
         for (int seg = 0;; ++seg) {
@@ -468,10 +469,11 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
                     for (int x = 0; x < kStepKeys; ++x) s[x] = __uint_as_float(su[x]);
 
                     // Hide what does not count: rows behind the end of a page's, and nodes that are no ancestors.  By a select, not by adding -inf: keys
-                    // that nobody sees may hold anything.
+                    // that nobody sees may hold anything.  Page by page: most steps have one page that is not full, if any.
                     if (!whole) {
 #pragma unroll
                         for (int e = 0; e < kStepPages; ++e) {
+                            if (pg[e] == kPageTokens) continue;
                             const uint32_t see = pg[e] & 256 ? static_cast<uint32_t>(tree >> (pg[e] & 63)) : (1u << pg[e]) - 1u;
 #pragma unroll
                             for (int x = 0; x < kPageTokens; ++x)
@@ -565,21 +567,34 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
                     l += (lo0 + hi0) + (lo1 + hi1);
                 }
                 if (ok && mine > 0) ok = mbar_wait(bar_o_done(i), static_cast<uint32_t>(on & 1), abort_flag, p.status);
-                // Both walkers' results of a row: references and sums go through shared memory, the accumulators lie in lanes that both warps
-                // read; each writes half of the channels.
+                // Both walkers' results of a row: walker 1 leaves reference and sum in shared memory, walker 0 what either's accumulator counts.  These
+                // lie in lanes that both warps read; each writes half of the channels.
                 if (mine == 0) { m = kNegInf; l = 0.f; }
-                ml[i * kTileRows + r] = make_float2(m, l);
-                tc_fence_before();
-                asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
-                tc_fence_after();
-                const float2 other = ml[(1 - i) * kTileRows + r];
-                asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");       // (the next segment's go to the same place)
-                const float top = fmaxf(m, other.x), mine_f = l > 0.f ? ex2(m - top) : 0.f, other_f = other.y > 0.f ? ex2(other.x - top) : 0.f;
-                const float sum = l * mine_f + other.y * other_f, inv = sum > 0.f ? 1.f / sum : 0.f;
-                const float f_mine = mine_f * inv, f_other = other_f * inv;
+                float f_mine, f_other;
                 const bool split = it.slot >= 0;
                 const long long slot = static_cast<long long>(it.slot) * p.row_tiles + rt;
-                if (split && i == 0) p.part_lse[slot * kTileRows + r] = sum > 0.f ? top + lg2(sum) : kNegInf;
+                tc_fence_before();
+                if (i == 1) {
+                    ml[r] = make_float2(m, l);
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                    const float2 f = ml[r];
+                    f_mine = f.y;
+                    f_other = f.x;
+                } else {
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                    const float2 other = ml[r];
+                    const float top = fmaxf(m, other.x);
+                    f_mine = l > 0.f ? ex2(m - top) : 0.f;
+                    f_other = other.y > 0.f ? ex2(other.x - top) : 0.f;
+                    const float sum = l * f_mine + other.y * f_other, inv = sum > 0.f ? 1.f / sum : 0.f;
+                    f_mine *= inv;
+                    f_other *= inv;
+                    ml[r] = make_float2(f_mine, f_other);
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                    if (split) p.part_lse[slot * kTileRows + r] = sum > 0.f ? top + lg2(sum) : kNegInf;
+                }
+                tc_fence_after();
                 // partial outputs [slot][D / 4][row][4]: a warp's store is one contiguous piece
                 float4 *part = reinterpret_cast<float4 *>(p.part_o) + slot * (D / 4) * kTileRows + r;
                 uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.out) +
