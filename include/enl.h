@@ -203,7 +203,7 @@ int enl_cache_status(enl_cache_t *c);
 int enl_cache_selfcheck(enl_cache_t *c);
 
 /*
- * Read-back of the gather plan built by the last enl_attend (host copy), for tests of the
+ * Read-back of the gather plan built by the last enl_attend or enl_attend_tree (host copy), for tests of the
  * integer book-keeping.  Each array pointer may be NULL; counts are always written.
  *   stream_pages[i], stream_meta[i] : page id and (slot << 8 | valid tokens) of KV-stream entry i
  *   ep_stream_off[b], ep_cached_tiles[b] : first entry and number of 128-key tiles of episode b

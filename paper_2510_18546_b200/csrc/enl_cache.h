@@ -102,6 +102,13 @@ struct KeyMapShape {
           box{64, static_cast<cuuint32_t>(box_rows(D)), static_cast<cuuint32_t>(D / 64), 1} {}
 };
 
+// What a plan of enl_attend_tree takes at most besides the streams: a segment per unit (request and kv head) and one more per CTA that runs at once.
+inline size_t tree_plan_bytes(int64_t batch, int64_t n_kv_heads)
+{
+    const size_t units = static_cast<size_t>(batch * n_kv_heads);
+    return (units + kTreeMaxPlaces) * (sizeof(TreeSegment) + sizeof(int32_t)) + units * sizeof(int2) + 256;
+}
+
 // pages of 16 rows, [n][Hkv][16][D]: a page of a head in one box
 struct PageMapShape {
     cuuint64_t dims[4], strides[3];
@@ -153,6 +160,7 @@ struct enl_cache {
     std::vector<int32_t> key_obj;           // object spans the row -> object map was built from
     bool plan_tree = false;                 // the plan is for enl_attend_tree: streams, and the CTAs' shares where there are several requests
     int32_t tree_rows = 0, tree_blocks = 0, tree_entries = 0;      // ... for this n_max and max_blocks; cached pages of a single request
+    std::vector<EpInfo> tree_eps;           // its episodes' streams (host only)
     int32_t tree_slots = 0;                 // partial results per tile of rows
     bool tree_ready = false;                // the kernel of enl_attend_tree has been opted in
     bool plan_decode = false;               // the plan is for the one-token decode kernel

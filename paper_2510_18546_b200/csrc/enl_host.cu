@@ -137,6 +137,7 @@ extern "C" int enl_cache_create(const enl_cache_desc_t *desc, enl_cache_t **out)
     auto align256 = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
     c->plan_bytes = align256(sizeof(EpInfo) * d.max_batch) + align256(sizeof(Item) * c->cap_items) +
                     2 * align256(sizeof(int32_t) * c->cap_entries) + align256(c->cap_entries / kPagesPerTile + 1) + 2 * align256(sizeof(int32_t) * d.max_q_tokens);
+    c->plan_bytes = std::max(c->plan_bytes, tree_plan_bytes(d.max_batch, d.n_kv_heads) + 2 * align256(sizeof(int32_t) * c->cap_entries));
     c->plan_layer_ok.assign(d.n_layers, 0);
 
     if (!c->gpu) {
@@ -1342,13 +1343,13 @@ extern "C" int enl_plan_inspect(const enl_cache_t *cc, int32_t cap_entries, int3
     if (n_entries) *n_entries = c->plan_entries;
     if (n_splits) *n_splits = c->plan_splits;
     if (n_items) *n_items = c->plan_items;
-    if (merge_kind) *merge_kind = c->plan_decode ? 3 : c->plan_pair ? 2 : c->plan_splits > 1 && !c->plan_mass_only ? 1 : 0;
+    if (merge_kind) *merge_kind = c->plan_tree ? (c->plan_splits > 1 ? 1 : 0) : c->plan_decode ? 3 : c->plan_pair ? 2 : c->plan_splits > 1 && !c->plan_mass_only ? 1 : 0;
     const int32_t *s = c->h_stream(), *m = c->h_meta();
     for (int i = 0; i < c->plan_entries && i < cap_entries; ++i) {
         if (stream_pages) stream_pages[i] = s[i];
         if (stream_meta) stream_meta[i] = m[i];
     }
-    const EpInfo *e = c->h_eps();
+    const EpInfo *e = c->plan_tree ? c->tree_eps.data() : c->h_eps();
     for (int b = 0; b < c->plan_batch && b < cap_batch; ++b) {
         if (ep_stream_off) ep_stream_off[b] = e[b].stream_off;
         if (ep_cached_tiles) ep_cached_tiles[b] = e[b].n_ctiles;

@@ -216,6 +216,7 @@ struct TreeMergeParams {
     int32_t row_groups;     // (filled in by the launcher)
 };
 constexpr int kTreeMaxNodes = 64;   // bits of a mask
+constexpr int kTreeMaxPlaces = 512; // CTAs that shares are made for, at most (the device's multiprocessors)
 cudaError_t prepare_tree(int head_dim);
 cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_t st);
 // most: parts of the unit that has most

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <new>
 #include <vector>
 
 #include "enl_cache.h"
@@ -11,10 +12,10 @@ using namespace enl;
 namespace {
 
 constexpr int kStepPages = kStepKeys / kPageTokens;
-// What calls take, in steps (of 64 keys) of a CTA while all CTAs run: 0.75 us, the memory's pace.
-constexpr double kMerge = 5.0;      // putting parts together
+// What calls take, in steps (of 64 keys, head_dim 128) of a CTA while all CTAs run: 0.75 us, the memory's pace.
+constexpr double kMerge = 5.0;      // putting parts together: 3.5 to 4 us between the end of the attention kernel and the next one's start
 constexpr double kSegment = 3.0;    // runs: another segment of a CTA
-constexpr double kPair = 1.7;      // a step of either walker where the memory is not what is waited for
+constexpr double kPair = 1.7;       // a step of either walker where the memory is not what is waited for (1.3 us)
 constexpr int kSegmentSteps = 2;    // runs do not begin or end closer to a unit's ends
 // Steps fetched before the wait for the previous kernel.  Where that is a merge kernel, whose loads they hold up, four if parts have kLongPart steps
 // and two if not (one token over 33 000 keys 29.9 us with two, 29.1 with four, 29.5 with six; 64 nodes over 7400 20.7, 21.2, 22.3).
@@ -106,7 +107,7 @@ struct Shares {
 
 }  // namespace
 
-extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, void *cuda_stream)
+static int attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, void *cuda_stream)
 {
     if (!c || !a) return ENL_E_INVAL;
     const enl_cache_desc_t &d = c->d;
@@ -160,7 +161,7 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         // Shares of the CTAs.  The host does not know how long the tails are, so they count for what their tables hold: too many parts of a stream
         // that turns out short cost little, since all CTAs run at once, one on a multiprocessor.
         const int64_t slot_bytes = static_cast<int64_t>(kTileRows) * (d.head_dim + 1) * 4 * row_tiles;
-        const int64_t places = std::max<int64_t>(1, c->n_sm / row_tiles), slots = d.scratch_bytes / slot_bytes;
+        const int64_t places = std::max<int64_t>(1, std::min(c->n_sm, kTreeMaxPlaces) / row_tiles), slots = d.scratch_bytes / slot_bytes;
         std::vector<int64_t> pages(B), parts(B), tried(B);
         for (int b = 0; b < B; ++b) {
             pages[b] = ceil_div(a->n_max, kPageTokens) + static_cast<int64_t>(a->max_blocks);
@@ -179,7 +180,9 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         sh.heads = d.n_kv_heads;
         int64_t n_groups = d.n_kv_heads * parts[0];
         if (B > 1) {
-            // Or runs, as long for every CTA, which cost most CTAs a second segment and most units a merge.
+            // Or runs, as long for every CTA, which cost most CTAs a second segment and most units a merge.  (16 requests of 3200 cached keys and
+            // tails of 256 to 768, 8 kv heads: 59.7 us in runs, 51.7 as 128 streams; what is better by the model has been measured at these
+            // sizes and at those of the tests only.)
             int64_t total = 0;
             std::vector<int64_t> steps(B);
             for (int b = 0; b < B; ++b) {
@@ -205,9 +208,9 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         c->off_meta = section(sizeof(int32_t) * n_entries);
         c->plan_used = at;
         int32_t ne = 0;
-        std::vector<EpInfo> eps(B);
+        std::vector<EpInfo> &eps = c->tree_eps;
+        eps.assign(B, EpInfo{});
         for (int b = 0; b < B; ++b) {
-            eps[b] = EpInfo{};
             eps[b].n_slots = cu_sel[b + 1] - cu_sel[b];
             ne = write_stream(c, eps[b], a->sel_ids + cu_sel[b], c->sel_len.data() + cu_sel[b], ne);
         }
@@ -312,4 +315,13 @@ extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, 
         if (launch_tree_merge(mp, d.head_dim, B, c->plan_splits, st) != cudaSuccess) { cudaGetLastError(); return ENL_E_CUDA; }
     }
     return ENL_OK;
+}
+
+extern "C" int enl_attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, void *cuda_stream)
+{
+    try {
+        return attend_tree(c, a, cuda_stream);
+    } catch (const std::bad_alloc &) {                      // of the host's lists: the plan is built anew by the next call
+        return ENL_E_NOMEM;
+    }
 }

@@ -178,6 +178,29 @@ def test_the_next_attention_need_not_wait_first(host):
     assert host.fake_kind(0) == ord("w") and host.fake_wait_first(1) == 1
 
 
+def test_plan_can_be_read_back(host):
+    """The same stream as enl_attend's for the same list, and how it is split."""
+    host.enl_plan_inspect.argtypes = enl.lib().enl_plan_inspect.argtypes
+
+    def inspect(c):
+        arr = [np.zeros(64, np.int32) for _ in range(4)]
+        n = [ctypes.c_int32() for _ in range(4)]
+        p = [x.ctypes.data_as(ctypes.c_void_p) for x in arr]
+        assert host.enl_plan_inspect(c.h, 64, p[0], p[1], ctypes.byref(n[0]), 64, p[2], p[3], ctypes.byref(n[1]), ctypes.byref(n[2]), ctypes.byref(n[3])) == enl.ENL_OK
+        return [x.tolist() for x in arr], [x.value for x in n]
+
+    c = Host(host)
+    assert c.attend() == enl.ENL_OK
+    streams, (entries, _, _, _) = inspect(c)
+    assert c.call() == enl.ENL_OK
+    mine, (e, splits, items, kind) = inspect(c)
+    assert mine[:2] == streams[:2] and mine[2][0] == streams[2][0] and mine[3][0] == streams[3][0] and e == entries
+    assert splits == host.fake_splits() and items == host.fake_grid() and kind == 1
+    assert c.call(sel=(0, 1, 2, 3), batch=2, cu_sel=np.array([0, 1, 4], np.int32)) == enl.ENL_OK
+    mine, _ = inspect(c)
+    assert mine[2][:2] == [0, 8] and mine[3][:2] == [1, 2]
+
+
 def test_a_captured_call_takes_its_plan_along(host):
     c = Host(host)
     assert c.call() == enl.ENL_OK
