@@ -14,7 +14,8 @@ namespace {
 constexpr int kStepPages = kStepKeys / kPageTokens;
 // What calls take, in steps (of 64 keys, head_dim 128) of a CTA while all CTAs run: 0.75 us, the memory's pace.
 constexpr double kMerge = 5.0;      // putting parts together: 3.5 to 4 us between the end of the attention kernel and the next one's start
-constexpr double kSegment = 3.0;    // runs: another segment of a CTA
+constexpr double kMergeRuns = 17.0; // the same for runs, which leave two parts a CTA, and what they lose besides
+constexpr int kSegment = 6;         // runs: another segment of a CTA (the accumulators read and written, a Q tile fetched, the first scores)
 constexpr double kPair = 1.7;       // a step of either walker where the memory is not what is waited for (1.3 us)
 constexpr int kSegmentSteps = 2;    // runs do not begin or end closer to a unit's ends
 // Steps fetched before the wait for the previous kernel.  Where that is a merge kernel, whose loads they hold up, four if parts have kLongPart steps
@@ -74,18 +75,19 @@ struct Shares {
                 }
         off.push_back(static_cast<int32_t>(segments.size()));
     }
-    // Runs of as many steps for every CTA, across units.  A run does not begin or end less than kSegmentSteps from a unit's own ends.
+    // Runs across units that take every CTA as long: as many steps, kSegment of them for the beginning of another unit.  A run does not begin or end
+    // less than kSegmentSteps from a unit's own ends.
     void runs(const std::vector<int64_t> &steps, int64_t groups)
     {
-        int64_t total = 0, at = 0, cut = 0, j = 0;         // steps of all units, before this unit, where run j ends
-        for (int64_t s : steps) total += s * heads;
+        int64_t total = 0, at = 0, j = 0;                  // of all units and before this one, beginnings counted; the run
+        for (int64_t s : steps) total += (s + kSegment) * heads;
         off.push_back(0);
         for (size_t b = 0; b < steps.size(); ++b)
             for (int h = 0; h < heads; ++h) {
                 const int64_t whole = steps[b];
                 int64_t from = 0;
                 for (;;) {
-                    cut = total * (j + 1) / groups - at;   // within this unit
+                    int64_t cut = total * (j + 1) / groups - at - kSegment;      // where run j ends, in steps of this unit
                     if (cut < from + kSegmentSteps && from > 0) cut = from;
                     if (cut < kSegmentSteps) cut = 0;
                     if (cut > whole - kSegmentSteps && cut < whole + kSegmentSteps) cut = whole;
@@ -98,7 +100,7 @@ struct Shares {
                     if (cut >= whole) break;
                 }
                 if (from < whole) add(static_cast<int>(b), h, from, whole, whole);
-                at += whole;
+                at += whole + kSegment;
             }
         if (off.back() != static_cast<int32_t>(segments.size())) off.push_back(static_cast<int32_t>(segments.size()));
     }
@@ -180,16 +182,17 @@ static int attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, void *cu
         sh.heads = d.n_kv_heads;
         int64_t n_groups = d.n_kv_heads * parts[0];
         if (B > 1) {
-            // Or runs, as long for every CTA, which cost most CTAs a second segment and most units a merge.  (16 requests of 3200 cached keys and
-            // tails of 256 to 768, 8 kv heads: 59.7 us in runs, 51.7 as 128 streams; what is better by the model has been measured at these
-            // sizes and at those of the tests only.)
+            // Or runs, as long for every CTA, which cost many CTAs a second segment and most units a merge.  Measured in equal parts and in runs (3200
+            // cached keys and tails of 256 to 768, 8 kv heads, 12 nodes, us): 7 requests 30.5 / 31.3, 10 42.8 / 40.5, 13 44.2 / 49.3, 16 45.0 / 56.1, 19
+            // 85.2 / 66.8, 24 87.9 / 80.0, 28 89.0 / 87.1, 32 90.4 / 98.9, 40 129.4 / 116.9; 800 cached keys: 10 20.5 / 24.4, 19 38.0 / 36.5, 24
+            // 39.2 / 39.5.
             int64_t total = 0;
             std::vector<int64_t> steps(B);
             for (int b = 0; b < B; ++b) {
                 steps[b] = steps_of(pages[b]);
-                total += steps[b] * d.n_kv_heads;
+                total += (steps[b] + kSegment) * d.n_kv_heads;
             }
-            const double by_runs = static_cast<double>(total) / places + kSegment + kMerge;
+            const double by_runs = static_cast<double>(total) / places + kMergeRuns;
             sh.units.assign(n_units, make_int2(0, 0));
             if (by_runs < by_parts && 2 * places <= slots) sh.runs(steps, places);
             else sh.equal(parts);

@@ -154,14 +154,14 @@ def test_one_long_request_among_short_ones():
     run((8, 2, 128), [[700] * 9, [20], [33], [16, 16]], [900, 3, 0, 17], [20, 20, 1, 7], 20)
 
 
-@pytest.mark.parametrize("model,batch,n_max", [((8, 2, 64), 80, 5), ((16, 2, 128), 79, 12), ((32, 2, 128), 27, 24), ((8, 2, 128), 76, 30)], ids=str)
+@pytest.mark.parametrize("model,batch,n_max", [((8, 2, 64), 40, 5), ((16, 2, 128), 41, 12), ((32, 2, 128), 14, 24), ((8, 2, 128), 40, 30)], ids=str)
 def test_runs_of_parts_across_requests(model, batch, n_max):
     """Streams that do not divide into equal parts: most CTAs take the end of one and the beginning of the next, with other counts of rows; some
     of them belong to requests that have ended or have no nodes, the first ones too."""
     rng = np.random.default_rng(n_max)
     tails, n_new = rng.integers(0, 300, batch), rng.integers(0, n_max + 1, batch)
     tails[::9], n_new[3::8] = -1, 0
-    c = Case(model, [[int(rng.integers(500, 800)) for _ in range(4)] for _ in range(batch)], tails, n_new, n_max, seed=n_max)
+    c = Case(model, [[int(rng.integers(900, 1200)) for _ in range(4)] for _ in range(batch)], tails, n_new, n_max, seed=n_max)
     try:
         c.call()
         tiles = -(-n_max * (model[0] // model[1]) // 128)
@@ -173,6 +173,21 @@ def test_runs_of_parts_across_requests(model, batch, n_max):
             c.call()
             torch.cuda.synchronize()
             assert torch.equal(first, c.out)
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("model,batch,n_max", [((8, 2, 64), 80, 5), ((8, 8, 128), 19, 9), ((32, 2, 128), 27, 24)], ids=str)
+def test_more_streams_than_multiprocessors(model, batch, n_max):
+    """More than a wave of CTAs, in whole streams or in runs."""
+    rng = np.random.default_rng(n_max)
+    tails, n_new = rng.integers(0, 300, batch), rng.integers(0, n_max + 1, batch)
+    tails[::9], n_new[3::8] = -1, 0
+    tails[-1], n_new[-1] = 100, n_max
+    c = Case(model, [[int(rng.integers(500, 800)) for _ in range(4)] for _ in range(batch)], tails, n_new, n_max, seed=n_max)
+    try:
+        c.call()
+        c.check()
     finally:
         c.close()
 
