@@ -67,7 +67,7 @@ enum {                                            /* return codes               
     ENL_E_CUDA     = -4,   /* a CUDA call failed, or a GPU operation on a bookkeeping cache    */
     ENL_E_TIMEOUT  = -5,   /* a bounded wait inside a kernel expired (see enl_cache_status and  */
                            /* enl_static_status)                                               */
-    ENL_E_LIMIT    = -6,   /* a size beyond the fixed maxima of enl_attend_static              */
+    ENL_E_LIMIT    = -6,   /* a size beyond the fixed maxima of an entry point                   */
                            /* -7 is not used                                                    */
     ENL_E_EVICTED  = -8,   /* the group's K/V is in the slow tier only (see enl_step_prepare)   */
     ENL_E_CORRUPT  = -9    /* enl_cache_selfcheck: a guard page of the pool has been written    */

@@ -1,4 +1,4 @@
-// Host side of the library: the paged per-group KV store, the gather plan and the four C-ABI calls.
+// Host side of the library: the paged per-group KV store, the gather plan and the C-ABI calls that go by it (enl_attend_tree: enl_tree.cu).
 // Everything here is integer book-keeping plus launches; all arithmetic of the method runs in kernels.
 #include <algorithm>
 #include <cstdio>
@@ -90,7 +90,7 @@ extern "C" const char *enl_strerror(int code)
         case ENL_E_NOMEM: return "out of pool pages, plan space or memory";
         case ENL_E_CUDA: return "CUDA error, or GPU operation on a bookkeeping-only cache";
         case ENL_E_TIMEOUT: return "a bounded wait inside a kernel expired";
-        case ENL_E_LIMIT: return "size beyond the fixed maxima of the entry point that allocates nothing";
+        case ENL_E_LIMIT: return "size beyond the fixed maxima of the entry point";
         case ENL_E_EVICTED: return "the group is in the slow tier only; enl_step_prepare loads it";
         case ENL_E_CORRUPT: return "a guard page of the pool has been written";
         default: return "unknown error";
