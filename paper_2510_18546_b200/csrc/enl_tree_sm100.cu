@@ -61,7 +61,7 @@ struct Cfg {
     static constexpr int kMlOff      = kVOff + kRingV * kStepBytes;      // [row] what the walkers tell each other
     static constexpr int kInfoOff    = kMlOff + kTileRows * 8;           // what the warps have to know of a segment, [2]
     static constexpr int kBarOff     = kInfoOff + 2 * 64;
-    static constexpr int kBars       = 15 + 2 * (kRingK + kRingV);
+    static constexpr int kBars       = 23 + 2 * (kRingK + kRingV);
     static constexpr int kSmemBytes  = kBarOff + 8 * kBars + 8;
     static_assert(kSmemBytes <= 233472 - 2 * 1024, "a CTA of the merge kernel beside it (each takes 1 KB for itself)");
 };
@@ -99,6 +99,9 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
     auto bar_k_empty = [&](int x) { return bar0 + 8u * (15 + C::kRingK + x); };
     auto bar_v_full  = [&](int x) { return bar0 + 8u * (15 + 2 * C::kRingK + x); };
     auto bar_v_empty = [&](int x) { return bar0 + 8u * (15 + 2 * C::kRingK + C::kRingV + x); };
+    const uint32_t bar1 = bar0 + 8u * (15 + 2 * (C::kRingK + C::kRingV));
+    auto bar_ml      = [&](int q) { return bar1 + 8u * q; };                     // walker 1's reference and sum of a quadrant's rows are there
+    auto bar_factors = [&](int q) { return bar1 + 8u * (4 + q); };               // and what walker 0 makes of them
     auto phase_of = [](int at, int places) { return static_cast<uint32_t>((at / places) & 1); };
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + C::kBarOff + 8 * C::kBars);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
@@ -157,21 +160,11 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
                      ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (threadIdx.x == 0) {
-        *abort_flag = 0;
-        mbar_init(bar_q_full, 2);                                 // the Q tile, the Info
-        mbar_init(bar_q_empty, 2 + 8);                            // both walkers' last Q K^T, every softmax warp's look at the Info
-        mbar_init(bar_o_free, 8);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(bar_pv_done(i), 1);
-            mbar_init(bar_o_done(i), 1);
-            for (int b = 0; b < 2; ++b) {
-                mbar_init(bar_s_full(i, b), 1);
-                mbar_init(bar_p_full(i, b), 4);                   // (a walker's first warp arrives for those without rows, too)
-            }
-        }
-        for (int x = 0; x < C::kRingK; ++x) { mbar_init(bar_k_full(x), 1); mbar_init(bar_k_empty(x), 1); }
-        for (int x = 0; x < C::kRingV; ++x) { mbar_init(bar_v_full(x), 1); mbar_init(bar_v_empty(x), 1); }
+    if (warp == 0) {
+        if (lane == 0) *abort_flag = 0;
+        // arrivals a phase: one, but for the Q tile and the Info; both walkers' last Q K^T and every softmax warp's look at the Info; the softmax
+        // warps that read the accumulators; those that write P (a walker's first warp arrives for the ones without rows, too)
+        for (int x = lane; x < C::kBars; x += 32) mbar_init(bar0 + 8u * x, x == 0 ? 2 : x == 1 ? 2 + 8 : x == 2 ? 8 : x >= 11 && x < 15 ? 4 : 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     tc_fence_before();
@@ -409,6 +402,7 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
         const float scale = p.scale_log2;
         float2 *ml = reinterpret_cast<float2 *>(smem + C::kMlOff);
         int f0 = 0, g0 = 0, on = 0;                                   // as for the issuers
+        int met = 0;                                                  // segments that this warp had rows in
         pdl_wait();
         for (int seg = 0;; ++seg) {
             ok = mbar_wait(bar_q_full, static_cast<uint32_t>(seg & 1), abort_flag, p.status);
@@ -574,15 +568,17 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
                 const bool split = it.slot >= 0;
                 const long long slot = static_cast<long long>(it.slot) * p.row_tiles + rt;
                 tc_fence_before();
+                const uint32_t meeting = static_cast<uint32_t>(met++ & 1);
                 if (i == 1) {
                     ml[r] = make_float2(m, l);
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                    __syncwarp();
+                    if (ok && lane == 0) mbar_arrive(bar_ml(q4));
+                    if (ok) ok = mbar_wait(bar_factors(q4), meeting, abort_flag, p.status);
                     const float2 f = ml[r];
                     f_mine = f.y;
                     f_other = f.x;
                 } else {
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                    if (ok) ok = mbar_wait(bar_ml(q4), meeting, abort_flag, p.status);
                     const float2 other = ml[r];
                     const float top = fmaxf(m, other.x);
                     f_mine = l > 0.f ? ex2(m - top) : 0.f;
@@ -591,7 +587,8 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
                     f_mine *= inv;
                     f_other *= inv;
                     ml[r] = make_float2(f_mine, f_other);
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + q4) : "memory");
+                    __syncwarp();
+                    if (ok && lane == 0) mbar_arrive(bar_factors(q4));
                     if (split) p.part_lse[slot * kTileRows + r] = sum > 0.f ? top + lg2(sum) : kNegInf;
                 }
                 tc_fence_after();
