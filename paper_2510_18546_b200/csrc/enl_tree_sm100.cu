@@ -743,19 +743,27 @@ cudaError_t launch_tree(const TreeParams &p, int head_dim, int grid, cudaStream_
     return e != cudaSuccess ? e : cudaGetLastError();
 }
 
+static int merge_row_groups(const TreeMergeParams &p, int lanes) { return (p.n_max * p.rep * lanes + kMergeWarps * 32 - 1) / (kMergeWarps * 32); }
 template <int D, int kLanes>
 static cudaError_t launch_merge(TreeMergeParams p, int batch, cudaStream_t st)
 {
-    constexpr int kRows = kMergeWarps * 32 / kLanes;
-    p.row_groups = (p.n_max * p.rep + kRows - 1) / kRows;
+    p.row_groups = merge_row_groups(p, kLanes);
     return launch_pdl(tree_merge_kernel<D, kLanes>, dim3(static_cast<unsigned>(batch) * p.Hkv * p.row_groups, D / 8), dim3(kMergeWarps * 32), 0, st, p);
 }
-// as many lanes a row as it takes to have all parts on their way at once
+// As many lanes a row as have two parts each, as long as the CTAs do not become more than 256 by it (there is room for one beside each of the attention
+// kernel's; the others come when that has ended).  With 2, 4 and 8 lanes (us a call, 32 / 8 heads but for the last two): 32 nodes in 4 parts 18.9 20.6 24.2, in
+// 14 10.5 11.4 12.0, in 16 32.0 33.0 33.8 (but over a third of the keys 21.4 20.8 20.7), 16 nodes in 11 10.3 10.2 10.7, one token in 16 31.0 29.5 29.2, in 11
+// 10.4 10.0 10.1, 4 kv heads, one token in 18 10.8 10.1 9.5, one kv head, 16 nodes in 120 17.5 13.7 11.9.  (With one lane 20.0 for the first and 13.9 for the last but one.)
 template <int D>
 static cudaError_t launch_merge(const TreeMergeParams &p, int batch, int most, cudaStream_t st)
 {
-    return most <= kMergeAhead ? launch_merge<D, 1>(p, batch, st) : most <= 2 * kMergeAhead ? launch_merge<D, 2>(p, batch, st)
-         : most <= 4 * kMergeAhead ? launch_merge<D, 4>(p, batch, st) : launch_merge<D, 8>(p, batch, st);
+    int lanes = 2;
+    while (lanes < 8 && 4 * lanes <= most) {
+        const int64_t groups = merge_row_groups(p, 2 * lanes);
+        if (groups > merge_row_groups(p, lanes) && groups * batch * p.Hkv * (D / 8) > 256) break;
+        lanes *= 2;
+    }
+    return lanes == 2 ? launch_merge<D, 2>(p, batch, st) : lanes == 4 ? launch_merge<D, 4>(p, batch, st) : launch_merge<D, 8>(p, batch, st);
 }
 cudaError_t launch_tree_merge(const TreeMergeParams &p, int head_dim, int batch, int most, cudaStream_t st)
 {
