@@ -183,9 +183,9 @@ static int attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, void *cu
         int64_t n_groups = d.n_kv_heads * parts[0];
         if (B > 1) {
             // Or runs, as long for every CTA, which cost many CTAs a second segment and most units a merge.  Measured in equal parts and in runs (3200
-            // cached keys and tails of 256 to 768, 8 kv heads, 12 nodes, us): 7 requests 30.5 / 31.3, 10 42.8 / 40.5, 13 44.2 / 49.3, 16 45.0 / 56.1, 19
-            // 85.2 / 66.8, 24 87.9 / 80.0, 28 89.0 / 87.1, 32 90.4 / 98.9, 40 129.4 / 116.9; 800 cached keys: 10 20.5 / 24.4, 19 38.0 / 36.5, 24
-            // 39.2 / 39.5.
+            // cached keys and tails of 256 to 768, 8 kv heads, 12 nodes, us): 7 requests 29.4 / 28.8, 10 42.6 / 38.4, 13 43.9 / 47.3, 16 45.1 / 53.8, 19
+            // 83.4 / 65.0, 24 87.6 / 78.0, 28 88.8 / 85.1, 32 90.5 / 97.9, 40 128.5 / 116.5; 800 cached keys: 10 20.6 / 23.6, 19 38.2 / 35.5, 24
+            // 39.3 / 37.8.
             int64_t total = 0;
             std::vector<int64_t> steps(B);
             for (int b = 0; b < B; ++b) {
