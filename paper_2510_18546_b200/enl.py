@@ -98,6 +98,7 @@ class EnlError(RuntimeError):
 
 _lib = None
 _native = None          # the _enl extension module
+_current_device = _device = None        # torch.cuda's: these calls have no cache that names their device, and are made with the tensors' as the current one
 _heads = {}             # cache handle -> (device, q heads, kv heads, head_dim): what the tensors of enl_attend_tree are checked against
 _n_layers = {}          # cache handle -> layer count (the all-layers store takes one pointer per layer)
 
@@ -170,12 +171,13 @@ def lib() -> ctypes.CDLL:
 
 def _binding():
     """The extension module (raises ImportError if it has not been built: there is no other path)."""
-    global _native
+    global _native, _current_device, _device
     if _native is None:
         lib()
         from . import _enl
         _enl.set_int32_converter(_i32)
         import torch
+        _current_device, _device = torch.cuda.current_device, torch.cuda.device
         _enl.set_types(torch.bfloat16, torch.int32, torch.int64, torch.Tensor, getattr(torch.Tensor, "__dlpack_c_exchange_api__", None))
         _native = _enl
     return _native
@@ -324,24 +326,18 @@ def enl_rope_rotate(rows, positions=None, first_pos: int = 0, base: float = 1000
         raise EnlError(rc, "enl_rope_rotate")
 
 
-def _on_device_of(t, call, *args) -> int:
-    """``call(device, *args)`` with the tensor's device as the current one (these calls have no cache that names it)."""
-    import torch
-    at = t.get_device()
-    if at < 0 or at == torch.cuda.current_device():
-        return call(at, *args)
-    with torch.cuda.device(at):
-        return call(at, *args)
-
-
 def enl_tail_tables(tail_len, block_table, n_blocks, free_pages, n_free, slots, positions=None, mask=None, n_new=None, parent=None,
                     pos_base=None, failed=None, stream: int = 0) -> None:
     """Room for the next rows of every request, and where they go.  Contiguous CUDA tensors, int32 but for ``mask`` (int64): ``tail_len``,
     ``n_blocks``, ``n_new``, ``pos_base`` ``[B]``, ``block_table`` ``[B, max_blocks]``, ``free_pages`` ``[n_pages]``, ``n_free`` and ``failed``
     ``[1]``, ``slots``, ``positions``, ``mask`` and ``parent`` ``[B, n_max]``.  ``block_table``, ``n_blocks``, ``free_pages`` and ``n_free`` are
     updated, ``slots``, ``positions`` and ``mask`` are results."""
-    rc = _on_device_of(slots, (_native or _binding()).tail_tables, tail_len, block_table, n_blocks, free_pages, n_free, slots, positions, mask,
-                       n_new, parent, pos_base, failed, stream or None)
+    native = _native or _binding()
+    at = slots.get_device()
+    if at >= 0 and at != _current_device():
+        with _device(at):
+            return enl_tail_tables(tail_len, block_table, n_blocks, free_pages, n_free, slots, positions, mask, n_new, parent, pos_base, failed, stream)
+    rc = native.tail_tables(at, tail_len, block_table, n_blocks, free_pages, n_free, slots, positions, mask, n_new, parent, pos_base, failed, stream or None)
     if rc != ENL_OK:
         raise EnlError(rc, "enl_tail_tables")
 
@@ -362,8 +358,12 @@ def enl_attend_tree(cache: int, layer: int, sel_ids: Sequence[int], q, k_new, v_
 def enl_tree_accept(parent, token, target, accept, n_accept, next_token, n_new=None, first=None, stream: int = 0) -> None:
     """Which drafted tokens the model would have written itself.  Contiguous int32 CUDA tensors: ``parent`` (None: a chain), ``token``, ``target``
     and ``accept`` ``[B, n_max]``, the others ``[B]``; ``accept``, ``n_accept`` and ``next_token`` are results."""
-    rc = _on_device_of(token, (_native or _binding()).tree_accept, parent, token, target, accept, n_accept, next_token, n_new, first,
-                       stream or None)
+    native = _native or _binding()
+    at = token.get_device()
+    if at >= 0 and at != _current_device():
+        with _device(at):
+            return enl_tree_accept(parent, token, target, accept, n_accept, next_token, n_new, first, stream)
+    rc = native.tree_accept(at, parent, token, target, accept, n_accept, next_token, n_new, first, stream or None)
     if rc != ENL_OK:
         raise EnlError(rc, "enl_tree_accept")
 
@@ -371,8 +371,12 @@ def enl_tree_accept(parent, token, target, accept, n_accept, next_token, n_new=N
 def enl_tail_append(ks, vs, k_tails, v_tails, slots, tail_len, tail_len_out, accept=None, n_accept=None, stream: int = 0) -> None:
     """Rows ``accept`` of every layer's ``ks`` and ``vs`` (``[B, n_max, Hkv, D]`` bf16, a contiguous CUDA tensor per layer) into its tail pages
     (``[n_pages, Hkv, 16, D]``) at ``slots`` ``[B, n_max]``; ``tail_len_out`` = ``tail_len`` + rows appended (it may be the same tensor)."""
-    rc = _on_device_of(slots, (_native or _binding()).tail_append, ks, vs, k_tails, v_tails, slots, tail_len, tail_len_out, accept, n_accept,
-                       stream or None)
+    native = _native or _binding()
+    at = slots.get_device()
+    if at >= 0 and at != _current_device():
+        with _device(at):
+            return enl_tail_append(ks, vs, k_tails, v_tails, slots, tail_len, tail_len_out, accept, n_accept, stream)
+    rc = native.tail_append(at, ks, vs, k_tails, v_tails, slots, tail_len, tail_len_out, accept, n_accept, stream or None)
     if rc != ENL_OK:
         raise EnlError(rc, "enl_tail_append")
 
