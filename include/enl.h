@@ -409,8 +409,8 @@ typedef struct {
  *   keys = the stored rows of the request's selected groups, the first tail_len[b] rows of its tail, and the nodes that mask[b][i] names;
  *   out  = softmax(q . keys / sqrt(head_dim)) . values         (fp32 accumulate, bf16 out)
  * A node that sees no key at all gets zeros.  Rows of `out` behind n_new[b], and those of a request whose tail_len is below zero, are
- * left as they are.  What lies in rows that do not count (behind a tail's end or the last node) may be anything; the V rows of the
- * request's own nodes have to be finite, those that a node does not see too.  A tail is taken to be max_blocks * 16 rows long at most, and an entry of the
+ * left as they are.  What lies in rows that do not count (behind a tail's end or the last node, or of nodes that a node does not see) may
+ * be anything, infinities and NaN among them.  A tail is taken to be max_blocks * 16 rows long at most, and an entry of the
  * block table that names no page reads as rows of zeros.  No masses: scoring is enl_attend's.
  * Limits on the select list are those of enl_attend.  Splits share the cache's scratch buffer: order the calls on one cache.
  * Errors: ENL_E_INVAL, ENL_E_NOGROUP, ENL_E_EVICTED, ENL_E_NOMEM (plan larger than the plan buffers), ENL_E_LIMIT (n_max, sizes that pass

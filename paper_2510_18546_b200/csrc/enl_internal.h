@@ -191,6 +191,7 @@ struct TreeParams {
     const int32_t *block_table;     // [batch][max_blocks] pages of the tails
     const int32_t *tail_len;        // [batch]
     const int32_t *n_new;           // [batch] nodes, or null: n_max
+    const void *v_new;              // as tm_vnew
     const unsigned long long *mask; // [batch][n_max] nodes that a node sees (a bit each), or null: a chain
     void   *out;            // bf16 [batch][n_max][Hq][D]
     float  *part_o;         // [slot][row tile][D / 4][128 rows][4] outputs of parts, normalised by their own sums

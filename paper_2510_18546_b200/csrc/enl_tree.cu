@@ -277,6 +277,7 @@ static int attend_tree(enl_cache_t *c, const enl_attend_tree_args_t *a, void *cu
     p.block_table = a->block_table;
     p.tail_len = a->tail_len;
     p.n_new = a->n_new;
+    p.v_new = a->v_new;
     p.mask = reinterpret_cast<const unsigned long long *>(a->mask);
     p.out = a->out;
     p.status = c->status_dev;

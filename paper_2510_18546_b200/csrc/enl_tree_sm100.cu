@@ -17,8 +17,8 @@
 // of its share of the memory; the tensor pipe needs 512 of them and the special-function units 512, but a walker's chain
 // scores -> softmax -> P V is 1600 long).  Hence two walkers, and shares that fill the device whatever the batch.  (Two CTAs per
 // multiprocessor with one walker each left twice as many partial results.)  In a chain of calls, 32 q / 8 kv heads, D = 128: 32 nodes over 33 000
-// keys 32.0 us (137 MB; 7.0 TB/s while the steps run, 12 us around them), one token 29.3, 64 nodes over 8500 keys 20.9 (a pair of steps 1.3 us),
-// 16 nodes over 2500 10.1, 16 requests of 24 nodes over 3800 46.3 (248 MB); 8 nodes over 192 keys, 8 / 2 heads, D = 64: 6.4.
+// keys 32.9 us (137 MB; 7.0 TB/s while the steps run, 13 us around them), one token 29.7, 64 nodes over 8500 keys 21.7 (a pair of steps 1.3 us),
+// 16 nodes over 2500 10.4, 16 requests of 24 nodes over 3800 46.5 (248 MB); 8 nodes over 192 keys, 8 / 2 heads, D = 64: 6.4.
 //
 // Shares: the host knows the cached pages of a request, but not how long its tail is.  So it cuts the stream of a request and kv head (a "unit")
 // by fractions: the part from a / E to b / E takes those pages of the C cached ones and the same part of the tail's and the nodes' pages, whose
@@ -70,6 +70,14 @@ struct Cfg {
 
 __device__ __forceinline__ int pages_of(int rows) { return (rows + kPageTokens - 1) / kPageTokens; }
 
+// two bf16: bits of those that are infinite or NaN; the finite ones alone
+__device__ __forceinline__ uint32_t odd_of(uint32_t w) { return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ void take_out(uint32_t &w)
+{
+    const uint32_t o = odd_of(w);
+    w &= ~((o >> 15 & 1u) * 0xffffu | (o >> 31) * 0xffff0000u);
+}
+
 // A segment as the warps behind the producers need it.
 struct Info {
     int b, kvh, slot;                         // request, kv head, slot of the partial results (-1: the whole)
@@ -78,8 +86,28 @@ struct Info {
     int tail_pages, len, n;                   // pages and rows of the whole tail, nodes
     int n_steps;
     int more;                                 // another segment follows
+    unsigned long long odd;                   // nodes with values that are not finite (the softmax warps add them)
 };
 static_assert(sizeof(Info) <= 64, "shared memory");
+
+// The rare case, kept out of the loop's registers: values of a page of nodes that are not finite become 0, their nodes are noted.
+template <int D>
+__device__ __noinline__ void take_out_of_page(uint8_t *page, int rows, int first, unsigned long long *odd)
+{
+    constexpr int kBlocks = D / 64, kGroupBytes = kBlocks * 1024;
+    for (int c = static_cast<int>(threadIdx.x & 31); c / (kBlocks * 8) < rows; c += 32) {
+        const int row = c / (kBlocks * 8);
+        uint4 *at = reinterpret_cast<uint4 *>(page + (row >> 3) * kGroupBytes + c / 8 % kBlocks * 1024 + (row & 7) * 128 + c % 8 * 16);
+        uint4 v = *at;
+        if (!(odd_of(v.x) | odd_of(v.y) | odd_of(v.z) | odd_of(v.w))) continue;
+        take_out(v.x);
+        take_out(v.y);
+        take_out(v.z);
+        take_out(v.w);
+        *at = v;
+        atomicOr(odd, 1ull << (first + row));
+    }
+}
 
 // (384 threads may have 168 registers; 144 leave room for a CTA of the merge kernel)
 template <int D>
@@ -242,7 +270,7 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
         };
         auto announce = [&](int si) {
             if (lane == 0) {
-                infos[(si - seg_beg) & 1] = Info{it.b, it.kvh, it.slot, it.first, it.count, t_first, t_count, tail_pages, len, n, n_steps, si + 1 < seg_end};
+                infos[(si - seg_beg) & 1] = Info{it.b, it.kvh, it.slot, it.first, it.count, t_first, t_count, tail_pages, len, n, n_steps, si + 1 < seg_end, 0ull};
                 mbar_arrive(bar_q_full);
             }
             __syncwarp();
@@ -532,26 +560,41 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
                         }
                         tmem_st16(t_sb + static_cast<uint32_t>(ch * 16), pk);
                     }
-                    // V rows that no row of the tile sees are cleared: 0 times whatever lies there must stay 0.  Those of the tail's last page and
-                    // behind the last node (pool pages are zero behind a group's end).
-                    if (!whole && q4 == 0) {
+                    // V rows that count for nobody are cleared: 0 times whatever lies there must stay 0.  Those behind a tail's end and behind the last
+                    // node (pool pages are zero behind a group's end).  For the same reason values of nodes that are not finite are taken out, for those
+                    // that do not see the node, and noted for those that do; the pages of nodes are dealt to the warps.  (Looking them over takes 0.1 to 1.0 us a call.)
+                    if (!whole && (2 * jj + i + 1) * kStepPages > it.count) {
                         const int f = f0 + 2 * jj + i, x = f % C::kRingV;
                         bool waited = false;
+                        auto dealt = [&](int e) { return n_act == 1 ? 0 : n_act == 2 ? e & 1 : n_act == 3 && e == 3 ? 0 : e; };
 #pragma unroll
                         for (int e = 0; e < kStepPages; ++e) {
-                            const int rows = pg[e] & 256 ? min(kPageTokens, n - (pg[e] & 63)) : pg[e];
-                            if ((2 * jj + i) * kStepPages + e < it.count || rows == 0 || rows == kPageTokens) continue;
+                            const bool nodes = (pg[e] & 256) != 0;
+                            const int first = pg[e] & 63, rows = nodes ? min(kPageTokens, n - first) : pg[e];
+                            if ((2 * jj + i) * kStepPages + e < it.count || rows == 0 || q4 != (nodes ? dealt(e) : 0) || (!nodes && rows == kPageTokens)) continue;
                             if (!waited) ok = mbar_wait(bar_v_full(x), phase_of(f, C::kRingV), abort_flag, p.status);
                             waited = true;
                             if (!ok) break;
                             uint8_t *page = smem + C::kVOff + x * C::kStepBytes + e * 2 * C::kGroupBytes;
-                            for (int c = lane; c < (kPageTokens - rows) * C::kBlocks * 8; c += 32) {    // 16-byte pieces
-                                const int row = rows + c / (C::kBlocks * 8), blk = c / 8 % C::kBlocks;
-                                *reinterpret_cast<uint4 *>(page + (row >> 3) * C::kGroupBytes + blk * 1024 + (row & 7) * 128 + c % 8 * 16) = make_uint4(0u, 0u, 0u, 0u);
+                            auto piece = [&](int c) {                     // of 16 bytes; eight of 64 channels of a row
+                                return reinterpret_cast<uint4 *>(page + (c / (C::kBlocks * 64)) * C::kGroupBytes + c / 8 % C::kBlocks * 1024 +
+                                                                 (c / (C::kBlocks * 8) & 7) * 128 + c % 8 * 16);
+                            };
+                            uint32_t found = 0;
+#pragma unroll
+                            for (int k = 0; k < kPageTokens * C::kBlocks / 4; ++k) {
+                                const int c = lane + 32 * k;
+                                if (c / (C::kBlocks * 8) >= rows) {
+                                    *piece(c) = make_uint4(0u, 0u, 0u, 0u);
+                                } else if (nodes) {
+                                    const uint4 v = *piece(c);
+                                    found |= odd_of(v.x) | odd_of(v.y) | odd_of(v.z) | odd_of(v.w);
+                                }
                             }
+                            if (__any_sync(kFull, found != 0)) take_out_of_page<D>(page, rows, first, &infos[seg & 1].odd);
                         }
                         if (!ok) break;
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        if (waited) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     }
                     tmem_st_wait();
                     tc_fence_before();
@@ -619,6 +662,24 @@ __global__ void __maxnreg__(144) tree_kernel(const __grid_constant__ TreeParams 
                         for (int x = 0; x < 2; ++x)
                             dst[k * 2 + x] = make_uint4(pack_bf16(f[8 * x], f[8 * x + 1]), pack_bf16(f[8 * x + 2], f[8 * x + 3]),
                                                         pack_bf16(f[8 * x + 4], f[8 * x + 5]), pack_bf16(f[8 * x + 6], f[8 * x + 7]));
+                    }
+                }
+                // What was taken out of the values that this row sees, into what this thread has written (noted by warps that have been waited for on the
+                // way here).
+                if (ok && row_valid) {
+                    for (unsigned long long left = *const_cast<volatile unsigned long long *>(&infos[seg & 1].odd) & tree; left; left &= left - 1) {
+                        const __nv_bfloat16 *v = static_cast<const __nv_bfloat16 *>(p.v_new) +
+                                                 ((static_cast<long long>(it.b) * p.n_max + __ffsll(left) - 1) * p.Hkv + it.kvh) * D;
+#pragma unroll 1
+                        for (int ch = i * (D / 2); ch < (i + 1) * (D / 2); ++ch) {
+                            const float add = __bfloat162float(v[ch]);
+                            if (fabsf(add) < INFINITY) continue;
+                            if (split) reinterpret_cast<float *>(part + (ch / 4) * kTileRows)[ch % 4] += add;
+                            else {
+                                __nv_bfloat16 *o = reinterpret_cast<__nv_bfloat16 *>(dst) + ch;
+                                *o = __float2bfloat16(__bfloat162float(*o) + add);
+                            }
+                        }
                     }
                 }
                 tc_fence_before();

@@ -269,6 +269,50 @@ def test_infinite_scores_and_values_of_hidden_keys():
         c.close()
 
 
+@pytest.mark.parametrize("model,tails,n_max", [((8, 2, 64), [40], 9), ((32, 8, 128), [0], 64), ((32, 8, 128), [700], 33), ((16, 1, 64), [5, 900, 0], 20),
+                                               ((4, 4, 128), [16, 3, 250, 64], 1), ((32, 2, 128), [100, 31], 50)], ids=str)
+def test_values_that_are_not_finite_reach_those_who_see_them(model, tails, n_max):
+    """0 x inf is NaN, but a node that is not seen does not count."""
+    c = Case(model, [[100, 30]] * len(tails), tails, [n_max] * len(tails), n_max, seed=n_max)
+    try:
+        rng = np.random.default_rng(n_max)
+        keep = c.v.clone()
+        what = np.zeros((c.batch, n_max, c.n_kv, c.d))
+        for _ in range(3 * c.batch):
+            b, j, h = int(rng.integers(c.batch)), int(rng.integers(n_max)), int(rng.integers(c.n_kv))
+            at = rng.choice(c.d, int(rng.choice([1, 5, c.d])), replace=False)
+            what[b, j, h, at] = rng.choice([NAN, np.inf, -np.inf])
+        odd = ~np.isfinite(what)
+        c.v = torch.where(dev(odd), dev(what, BF16), c.v)
+        clean = torch.where(dev(odd), torch.zeros_like(keep), keep)
+        c.call()
+        torch.cuda.synchronize()
+        assert enl.enl_cache_status(c.cache) == enl.ENL_OK
+        got, rep = f64(c.out), c.n_q // c.n_kv
+        with np.errstate(invalid="ignore"):
+            for b in range(c.batch):
+                for i in range(n_max):
+                    seen = np.nonzero(c.see[b][i])[0]
+                    add = np.repeat(np.where(odd[b, seen], what[b, seen], 0.0).sum(0), rep, 0)      # 0, inf, -inf or NaN for every head and channel
+                    bad = ~np.isfinite(add)
+                    assert np.array_equal(got[b, i][bad], add[bad], equal_nan=True)
+                    assert np.isfinite(got[b, i][~bad]).all()
+                    got[b, i][bad] = 0.0
+        # where they are finite, outputs are those of the same values without them
+        c.v = clean
+        c.call()
+        torch.cuda.synchronize()
+        want = f64(c.out)
+        for b in range(c.batch):
+            for i in range(n_max):
+                seen = np.nonzero(c.see[b][i])[0]
+                bad = np.repeat(odd[b, seen].any(0), rep, 0)
+                assert np.array_equal(got[b, i][~bad], want[b, i][~bad])
+        c.check()
+    finally:
+        c.close()
+
+
 def test_small_scratch_means_no_splits():
     run((8, 2, 128), [[300] * 4], [200], [8], 8, scratch_bytes=4096)
     run((8, 2, 128), [[300] * 4] * 3, [200, 0, 9], [8, 1, 3], 8, scratch_bytes=200000)
